@@ -156,6 +156,35 @@ typedef struct {
   const void *w_m, *b_m;       /* [6D][D], [6D] */
 } ardit_time_weights;
 
+/* Format of the codes of a microscaled KV cache. */
+typedef enum {
+  ARDIT_KV_E4M3 = 1,   /* 8 bits: OCP FP8 E4M3 */
+  ARDIT_KV_E2M1 = 2    /* 4 bits: OCP FP4 E2M1; of two codes in a byte the first has the low half */
+} ardit_kv_format;
+
+/* Frame-paged KV cache of one layer held in 8 or 4 bits (device memory): blocks
+ * of 32 values share a power of two 2^e, and a code c stands for c 2^e.  Blocks
+ * run along each attention product's summed axis: 32 dims of a token's head
+ * (keys), 32 keys of a page, per dim (values; a page's last block may hold
+ * fewer).  e is the smallest exponent, at least -117, with max|x| / 2^e below 256
+ * (E4M3) or at most 6 (E2M1), so that no code saturates; its byte is e + 127, and
+ * 255 marks a block that held an infinity or NaN, every value of which reads back
+ * as NaN.  Codes are rounded to nearest, ties to even.  Every value is exact in
+ * bf16.
+ * A page holds tiles of 64 keys: with T64 = T rounded up to 64 and n = T64 / 64,
+ *   k_codes  [n_pages][H][T64][d] codes      k_scales [n_pages][H][T64][d / 32]
+ *   v_codes  [n_pages][H][n][d][64] codes    v_scales [n_pages][H][n][2][d]
+ * (ardit_kv_mx_bytes gives the sizes).  Keys past T are padding: no result
+ * depends on what is there. */
+typedef struct {
+  void *k_codes, *k_scales;    /* 16-byte aligned */
+  void *v_codes, *v_scales;
+  const int32_t* page_table;   /* as in ardit_kv_paged, like the three below */
+  int32_t n_pages;
+  int32_t max_frames;
+  int32_t format;              /* ardit_kv_format */
+} ardit_kv_mx;
+
 /* Name of a status code; never NULL. */
 const char* ardit_status_str(int status);
 /* Detail of the calling thread's last failed call ("" if none). */
@@ -247,6 +276,45 @@ int ardit_attn_fwd_noalloc(hipStream_t stream, const ardit_dims* dims, const ard
  * x / 2^e (|x / 2^e| < 256, no saturation).  cols % 32 == 0. */
 int ardit_mx_quantize(hipStream_t stream, const void* x, int64_t rows, int32_t cols, int32_t ld,
                       void* codes, void* scales);
+
+/* Bytes of the codes, and of the scales, of the keys of n_pages pages of a
+ * microscaled cache (the values take as many each): n_pages H T64 d, or half of
+ * it in E2M1, and n_pages H T64 d / 32.  Host only. */
+int ardit_kv_mx_bytes(const ardit_dims* dims, int32_t format, int32_t n_pages, size_t* code_bytes,
+                      size_t* scale_bytes);
+
+/* ardit_kv_append into a microscaled cache: q~ and the chunk's k~ and v as there
+ * (norm, rotation and scaling in fp32, the rotation's angles in fp64), k~ and v
+ * quantised from their fp32 values into slots [cache_len, cache_len + q_len) of
+ * the stream's pages.  The values' padding in the tiles written becomes zero;
+ * nothing else of the pool is written.  Chunks of whole frames, as there. */
+int ardit_kv_append_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                       const void* qkv, const void* g_q, const void* g_k, const ardit_kv_mx* kv,
+                       void* q_out);
+
+/* Reads keys and values of a microscaled cache back into bf16 pages, exactly:
+ * logical tokens [cache_len, cache_len + q_len) of each stream of src (the slots
+ * that an append of the same batch writes; cache_lens 0 and q_lens n for a
+ * history of n tokens) go to the same logical tokens of dst, through dst's own
+ * page table.  q_lens need not be whole frames: tokens of dst past them stay as
+ * they are.  Table entries of other frames are not read; a dst entry outside its
+ * pool drops that frame.  The two pools must not overlap. */
+int ardit_kv_read_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                     const ardit_kv_mx* src, const ardit_kv_paged* dst);
+
+/* ardit_attn_fwd over a microscaled cache: o = softmax(q K^T / sqrt(d)) V with K, V
+ * the values the codes stand for and q in bf16, not quantised; any q_lens.  All
+ * streams bf16 and dense (batch->quant and batch->sparsity: ARDIT_EUNSUPPORTED
+ * otherwise).  shared_frames > 0 says that the batch continues one history: the
+ * first shared_frames table entries of every stream that has queries are the
+ * same (with ardit_debug_checks(1) ARDIT_EINVAL otherwise), and each such stream
+ * caches at least those frames (ARDIT_ESHAPE); their pages are then read once for the rows
+ * of all streams where that saves work.  Few rows are split over their keys, and
+ * the schedule depends on the whole batch, as in ardit_attn_fwd.  ws / ws_bytes:
+ * ardit_workspace_size of this batch. */
+int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                      const void* q, const ardit_kv_mx* kv, int32_t shared_frames, void* o, void* ws,
+                      size_t ws_bytes);
 
 /* Block selection of block-sparse self-attention (paper, Section 2.1: the
  * sparsity knob rho skips attention blocks a sparse mask leaves out; Section 5

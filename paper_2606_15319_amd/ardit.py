@@ -62,6 +62,12 @@ class ardit_kv_paged(C.Structure):
                 ("n_pages", C.c_int32), ("max_frames", C.c_int32)]
 
 
+class ardit_kv_mx(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p),
+                ("v_scales", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("max_frames", C.c_int32), ("format", C.c_int32)]
+
+
 _BLOCK_FIELDS = ("w_qkv", "b_qkv", "g_q", "g_k", "w_o", "b_o", "g_n3", "w_cq", "b_cq", "g_cq",
                  "w_ck", "b_ck", "g_ck", "w_cv", "b_cv", "w_co", "b_co", "w_1", "b_1", "w_2",
                  "b_2", "mod_table")
@@ -108,6 +114,13 @@ _SIGS = {
     "ardit_attn_fwd_noalloc": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp,
                                          _P(ardit_kv_paged), _vp]),
     "ardit_mx_quantize": (C.c_int, [_vp, _vp, C.c_int64, _i32, _i32, _vp, _vp]),
+    "ardit_kv_mx_bytes": (C.c_int, [_P(ardit_dims), _i32, _i32, _P(_sz), _P(_sz)]),
+    "ardit_kv_append_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp, _vp, _vp,
+                                     _P(ardit_kv_mx), _vp]),
+    "ardit_kv_read_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _P(ardit_kv_mx),
+                                   _P(ardit_kv_paged)]),
+    "ardit_attn_fwd_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp, _P(ardit_kv_mx),
+                                    _i32, _vp, _vp, _sz]),
     "ardit_sparse_select": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp,
                                       _P(ardit_kv_paged), _vp, _i32, _vp, _sz]),
     "ardit_block_fwd": (C.c_int, [_vp, _P(ardit_dims), _vp, ardit_kv_paged, _i32, _i32, _vp,
@@ -238,6 +251,12 @@ def kv_paged(k_pages, v_pages, page_table, n_pages: int, max_frames: int) -> ard
                           int(max_frames))
 
 
+def kv_mx(k_codes, k_scales, v_codes, v_scales, page_table, n_pages: int, max_frames: int,
+          fmt: int) -> ardit_kv_mx:
+    return ardit_kv_mx(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
+                       _ptr(page_table), int(n_pages), int(max_frames), int(fmt))
+
+
 def block_weights(w: dict) -> ardit_block_weights:
     return ardit_block_weights(*[_ptr(w.get(n)) for n in _BLOCK_FIELDS])
 
@@ -289,6 +308,35 @@ QUANT_BF16, QUANT_FP8 = 0, 1
 def ardit_mx_quantize(stream, x, rows, cols, ld, codes, scales):
     _check(_lib.ardit_mx_quantize(_stream(stream), _ptr(x), int(rows), int(cols), int(ld),
                                   _ptr(codes), _ptr(scales)), "ardit_mx_quantize")
+
+
+KV_E4M3, KV_E2M1 = 1, 2
+
+
+def ardit_kv_mx_bytes(dims, fmt: int, n_pages: int):
+    """(code bytes, scale bytes) of the keys, and of the values, of n_pages pages."""
+    c, s = C.c_size_t(0), C.c_size_t(0)
+    _check(_lib.ardit_kv_mx_bytes(C.byref(dims), int(fmt), int(n_pages), C.byref(c), C.byref(s)),
+           "ardit_kv_mx_bytes")
+    return c.value, s.value
+
+
+def ardit_kv_append_mx(stream, dims, batch: Batch, qkv, g_q, g_k, kv: ardit_kv_mx, q_out):
+    _check(_lib.ardit_kv_append_mx(_stream(stream), C.byref(dims), C.byref(batch.struct),
+                                   _ptr(qkv), _ptr(g_q), _ptr(g_k), C.byref(kv), _ptr(q_out)),
+           "ardit_kv_append_mx")
+
+
+def ardit_kv_read_mx(stream, dims, batch: Batch, src: ardit_kv_mx, dst: ardit_kv_paged):
+    _check(_lib.ardit_kv_read_mx(_stream(stream), C.byref(dims), C.byref(batch.struct),
+                                 C.byref(src), C.byref(dst)), "ardit_kv_read_mx")
+
+
+def ardit_attn_fwd_mx(stream, dims, batch: Batch, q, kv: ardit_kv_mx, shared_frames: int, o, ws,
+                      ws_bytes):
+    _check(_lib.ardit_attn_fwd_mx(_stream(stream), C.byref(dims), C.byref(batch.struct), _ptr(q),
+                                  C.byref(kv), int(shared_frames), _ptr(o), _ptr(ws),
+                                  int(ws_bytes)), "ardit_attn_fwd_mx")
 
 
 def ardit_sparse_select(stream, dims, batch: Batch, q, kv: ardit_kv_paged, blocks, row_stride,

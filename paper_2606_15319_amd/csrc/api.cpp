@@ -228,25 +228,72 @@ int check_sparse(const ardit_dims* d, const ardit_batch* b) {
   return ARDIT_OK;
 }
 
+// The pool's size and the rows of its page table against what the batch needs.
+int check_pool(const ardit_dims* d, const ardit_batch* b, int32_t n_pages, int32_t max_frames) {
+  if (n_pages < 1 || max_frames < 1)
+    return fail(ARDIT_EINVAL, "n_pages and max_frames must be >= 1");
+  const int64_t T = tokens_per_frame(d);
+  if (static_cast<int64_t>(n_pages) * d->dim * T > (int64_t(1) << 40))
+    return fail(ARDIT_ECAPACITY, "page pool too large");
+  for (int i = 0; i < b->n_streams; ++i) {
+    const int64_t keys = static_cast<int64_t>(b->cache_lens[i]) + b->q_lens[i];
+    const int64_t frames = (keys + T - 1) / T;
+    if (frames > max_frames)
+      return fail(ARDIT_ECAPACITY, "stream %d needs %lld frames > max_frames %d", i,
+                  static_cast<long long>(frames), max_frames);
+  }
+  return ARDIT_OK;
+}
+
 int check_kv(const ardit_dims* d, const ardit_batch* b, const ardit_kv_paged* kv) {
   if (!kv) return fail(ARDIT_EINVAL, "kv is NULL");
   if (!kv->k_pages || !kv->v_pages || !kv->page_table)
     return fail(ARDIT_EINVAL, "kv pointers must be non-NULL");
   if (misaligned(kv->k_pages) || misaligned(kv->v_pages))
     return fail(ARDIT_EINVAL, "kv pages must be 16-byte aligned");
-  if (kv->n_pages < 1 || kv->max_frames < 1)
-    return fail(ARDIT_EINVAL, "n_pages and max_frames must be >= 1");
-  const int64_t T = tokens_per_frame(d);
-  if (static_cast<int64_t>(kv->n_pages) * d->dim * T > (int64_t(1) << 40))
-    return fail(ARDIT_ECAPACITY, "page pool too large");
-  for (int i = 0; i < b->n_streams; ++i) {
-    const int64_t keys = static_cast<int64_t>(b->cache_lens[i]) + b->q_lens[i];
-    const int64_t frames = (keys + T - 1) / T;
-    if (frames > kv->max_frames)
-      return fail(ARDIT_ECAPACITY, "stream %d needs %lld frames > max_frames %d", i,
-                  static_cast<long long>(frames), kv->max_frames);
-  }
+  return check_pool(d, b, kv->n_pages, kv->max_frames);
+}
+
+int check_format(int32_t format) {
+  if (format != ARDIT_KV_E4M3 && format != ARDIT_KV_E2M1)
+    return fail(ARDIT_EINVAL, "%d is not a format of the microscaled cache", format);
   return ARDIT_OK;
+}
+
+int check_kv_mx(const ardit_dims* d, const ardit_batch* b, const ardit_kv_mx* kv) {
+  if (!kv) return fail(ARDIT_EINVAL, "kv is NULL");
+  if (!kv->k_codes || !kv->k_scales || !kv->v_codes || !kv->v_scales || !kv->page_table)
+    return fail(ARDIT_EINVAL, "kv pointers must be non-NULL");
+  if (misaligned(kv->k_codes) || misaligned(kv->k_scales) || misaligned(kv->v_codes) ||
+      misaligned(kv->v_scales))
+    return fail(ARDIT_EINVAL, "kv codes and scales must be 16-byte aligned");
+  ARDIT_TRY(check_format(kv->format));
+  ARDIT_TRY(check_pool(d, b, kv->n_pages, kv->max_frames));
+  // tiles are counted, and keys with their padding addressed, in 32 bits
+  const int64_t T = tokens_per_frame(d), nt = (T + kAttnKTile - 1) / kAttnKTile;
+  for (int i = 0; i < b->n_streams; ++i)
+    if (kAttnKTile * mx_tiles(static_cast<int64_t>(b->cache_lens[i]) + b->q_lens[i], T, nt) >= (int64_t(1) << 31))
+      return fail(ARDIT_ECAPACITY, "stream %d: its keys padded to tiles reach 2^31", i);
+  return ARDIT_OK;
+}
+
+MxPages mx_pages(const ardit_dims* d, const ardit_kv_mx* kv) {
+  MxPages p;
+  p.k = static_cast<uint8_t*>(kv->k_codes);
+  p.ks = static_cast<uint8_t*>(kv->k_scales);
+  p.v = static_cast<uint8_t*>(kv->v_codes);
+  p.vs = static_cast<uint8_t*>(kv->v_scales);
+  p.page_table = kv->page_table;
+  p.max_frames = kv->max_frames;
+  p.n_pages = kv->n_pages;
+  p.T = tokens_per_frame(d);
+  p.nt = (p.T + kAttnKTile - 1) / kAttnKTile;
+  p.H = d->n_heads;
+  p.hd = d->head_dim;
+  p.bits = kv->format == ARDIT_KV_E4M3 ? 8 : 4;
+  p.fT = make_fastdiv(p.T);
+  p.fnt = make_fastdiv(p.nt);
+  return p;
 }
 
 // Opt-in validation of the page tables against the pool (ardit_debug_checks).
@@ -255,8 +302,11 @@ std::atomic<int> g_debug_checks{0};
 // With the debug checks on: copies the page table to the host (synchronising
 // `st`) and checks every entry a stream reads or writes against the pool, and
 // that no page the batch writes is used by another stream or twice.
+// `from_chunk`: only the frames from cache_len on are used.  `shared`: the first
+// entries that all streams with queries must have in common.
+template <typename KV>
 int check_pages(hipStream_t st, const ardit_dims* d, const ardit_batch* b,
-                const ardit_kv_paged* kv, bool writes) {
+                const KV* kv, bool writes, bool from_chunk = false, int32_t shared = 0) {
   if (!g_debug_checks.load(std::memory_order_relaxed)) return ARDIT_OK;
   const int64_t T = tokens_per_frame(d);
   const size_t n = static_cast<size_t>(b->n_streams) * kv->max_frames;
@@ -265,11 +315,19 @@ int check_pages(hipStream_t st, const ardit_dims* d, const ardit_batch* b,
                            hipMemcpyDeviceToHost, st), "page table copy");
   ARDIT_HIP(hipStreamSynchronize(st), "page table copy");
   std::vector<int32_t> owner(static_cast<size_t>(kv->n_pages), -1);   // stream writing the page
+  int first = 0;
+  while (first < b->n_streams && b->q_lens[first] == 0) ++first;
+  for (int i = first + 1; i < b->n_streams; ++i)
+    for (int32_t f = 0; f < shared && b->q_lens[i] > 0; ++f)
+      if (table[static_cast<size_t>(i) * kv->max_frames + f] !=
+          table[static_cast<size_t>(first) * kv->max_frames + f])
+        return fail(ARDIT_EINVAL, "frame %d of streams %d and %d, within the %d shared, has two pages", f,
+                    first, i, shared);
   for (int i = 0; i < b->n_streams; ++i) {
     if (b->q_lens[i] == 0) continue;
     const int64_t keys = static_cast<int64_t>(b->cache_lens[i]) + b->q_lens[i];
     const int64_t frames = (keys + T - 1) / T;
-    for (int64_t f = 0; f < frames; ++f) {
+    for (int64_t f = from_chunk ? b->cache_lens[i] / T : 0; f < frames; ++f) {
       const int32_t p = table[static_cast<size_t>(i) * kv->max_frames + f];
       if (p < 0 || p >= kv->n_pages)
         return fail(ARDIT_ECAPACITY, "stream %d frame %lld: page %d outside the pool of %d", i,
@@ -281,7 +339,7 @@ int check_pages(hipStream_t st, const ardit_dims* d, const ardit_batch* b,
       }
     }
   }
-  if (writes)
+  if (writes && !from_chunk)
     for (int i = 0; i < b->n_streams; ++i) {
       if (b->q_lens[i] == 0) continue;
       const int64_t cached = b->cache_lens[i] / T;
@@ -666,6 +724,37 @@ AttnArgs cross_attn_args(const ardit_dims* d, const ardit_batch* b, const void* 
   }
   plan_attention(a, d->head_dim, split_ws);
   return a;
+}
+
+// ------------------------------------------------ microscaled key/value pages
+// streams that attend to a microscaled cache run bf16, dense attention
+int check_mx_streams(const ardit_batch* b) {
+  if (batch_sparse(b))
+    return fail(ARDIT_EUNSUPPORTED, "block-sparse attention needs a bf16 cache");
+  if (batch_fp8(b))
+    return fail(ARDIT_EUNSUPPORTED, "FP8 attention needs a bf16 cache");
+  return ARDIT_OK;
+}
+
+int append_mx(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* qkv,
+              const void* g_q, const void* g_k, const ardit_kv_mx* kv, void* q_out) {
+  const RopeGeom rg{d->dim, d->n_heads, d->head_dim, tokens_per_frame(d), d->lat_w,
+                    kv->max_frames, kv->n_pages, d->eps, d->rope_theta};
+  ARDIT_TIMED(kTimeElem,
+              launch_kv_append_mx(st, static_cast<const bf16_t*>(qkv), static_cast<int>(sum_q(b)), rg,
+                                  static_cast<const bf16_t*>(g_q), static_cast<const bf16_t*>(g_k),
+                                  static_cast<bf16_t*>(q_out), mx_pages(d, kv), q_streams(b)),
+              "qk_norm_rope / microscaled kv append");
+  return ARDIT_OK;
+}
+
+int attention_mx(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* q,
+                 const ardit_kv_mx* kv, int32_t shared, void* o, void* ws, const Ws& L) {
+  ARDIT_TIMED(kTimeAttn,
+              launch_attention_mx(st, mx_pages(d, kv), static_cast<const bf16_t*>(q),
+                                  static_cast<bf16_t*>(o), q_streams(b), shared, at<float>(ws, L.attn)),
+              "microscaled self-attention launch");
+  return ARDIT_OK;
 }
 
 // the block chain on validated arguments
@@ -1054,6 +1143,77 @@ int ardit_mx_quantize(hipStream_t stream, const void* x, int64_t rows, int32_t c
                                     static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales)),
             "mx quantisation launch");
   return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_kv_mx_bytes(const ardit_dims* dims, int32_t format, int32_t n_pages, size_t* code_bytes,
+                      size_t* scale_bytes) try {
+  ARDIT_TRY(check_dims(dims));
+  ARDIT_TRY(check_format(format));
+  if (n_pages < 1) return fail(ARDIT_EINVAL, "n_pages must be >= 1");
+  if (!code_bytes || !scale_bytes) return fail(ARDIT_EINVAL, "sizes must be non-NULL");
+  const size_t keys = static_cast<size_t>(ceil_div(tokens_per_frame(dims), kAttnKTile)) * kAttnKTile;
+  const size_t values = static_cast<size_t>(n_pages) * keys * dims->dim;
+  *code_bytes = format == ARDIT_KV_E4M3 ? values : values / 2;
+  *scale_bytes = values / 32;
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_kv_append_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                       const void* qkv, const void* g_q, const void* g_k, const ardit_kv_mx* kv,
+                       void* q_out) try {
+  ARDIT_TRY(check_dims(dims));
+  ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache | kUsePos | kChunkQ));
+  ARDIT_TRY(check_kv_mx(dims, batch, kv));
+  ARDIT_TRY(check_ptr(qkv, "qkv"));
+  ARDIT_TRY(check_ptr(g_q, "g_q"));
+  ARDIT_TRY(check_ptr(g_k, "g_k"));
+  ARDIT_TRY(check_ptr(q_out, "q_out"));
+  ARDIT_TRY(check_pages(stream, dims, batch, kv, true));
+  return append_mx(stream, dims, batch, qkv, g_q, g_k, kv, q_out);
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_kv_read_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                     const ardit_kv_mx* src, const ardit_kv_paged* dst) try {
+  ARDIT_TRY(check_dims(dims));
+  ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache));
+  ARDIT_TRY(check_kv_mx(dims, batch, src));
+  ARDIT_TRY(check_kv(dims, batch, dst));
+  ARDIT_TRY(check_pages(stream, dims, batch, src, false, true));
+  ARDIT_TRY(check_pages(stream, dims, batch, dst, true, true));
+  ARDIT_HIP(launch_kv_read_mx(stream, mx_pages(dims, src), static_cast<bf16_t*>(dst->k_pages),
+                              static_cast<bf16_t*>(dst->v_pages), dst->page_table, dst->max_frames,
+                              dst->n_pages, q_streams(batch)),
+            "microscaled read-back launch");
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                      const void* q, const ardit_kv_mx* kv, int32_t shared_frames, void* o, void* ws,
+                      size_t ws_bytes) try {
+  ARDIT_TRY(check_dims(dims));
+  ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache));
+  ARDIT_TRY(check_kv_mx(dims, batch, kv));
+  ARDIT_TRY(check_mx_streams(batch));
+  if (shared_frames < 0) return fail(ARDIT_EINVAL, "shared_frames %d is negative", shared_frames);
+  for (int i = 0; i < batch->n_streams; ++i)
+    if (batch->q_lens[i] > 0 &&
+        static_cast<int64_t>(shared_frames) * tokens_per_frame(dims) > batch->cache_lens[i])
+      return fail(ARDIT_ESHAPE, "stream %d caches %d tokens, fewer than the %d frames shared", i,
+                  batch->cache_lens[i], shared_frames);
+  ARDIT_TRY(check_ptr(q, "q"));
+  ARDIT_TRY(check_ptr(o, "o"));
+  Ws L;
+  ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
+  ARDIT_TRY(check_pages(stream, dims, batch, kv, false, false, shared_frames));
+  return attention_mx(stream, dims, batch, q, kv, shared_frames, o, ws, L);
 } catch (...) {
   return host_failure();
 }

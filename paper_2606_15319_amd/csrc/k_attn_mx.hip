@@ -1,0 +1,477 @@
+// Attention over microscaled key/value pages on gfx950.
+//
+// o = softmax(q K^T / sqrt(d)) V per (stream, head) over keys [0, kv_len), K and
+// V the values that the pages' codes stand for (mx.h), q and o bf16.
+//
+// Scores.  Keys go into the matrix cores as they lie in the pages: the scaled
+// product v_mfma_scale_f32_32x32x64_f8f6f4 takes E4M3 or E2M1 codes and applies a
+// scale byte per 32 of its 64 steps.  The queries keep their 8 bits: a bf16 number
+// is hi + lo with hi its four leading significant bits and lo the rest, both E4M3
+// (hi with the block's scale, lo with one 2^-4 smaller; below 2^-13 of the block's
+// largest element lo runs out of bits, an error of 2^-21 of that element).  Two
+// products at twice bf16's rate, so the time of one in bf16, and the keys are never
+// converted nor stored twice as wide.
+//   S^T = K Q_hi^T + K Q_lo^T (32 keys x 32 queries a product).
+// Weights.  exp2 in fp32 against a running maximum, rounded to bf16 (2^-9 of a
+// weight at most, errors of both signs: about 1e-3 of an output), summed as rounded.
+//   O^T += V^T P^T on v_mfma_f32_32x32x16_bf16, V converted to bf16 (exact).
+//
+// Operand layouts (measured): of the scaled product, lane m + 32 h holds row m and,
+// of E4M3, steps 16 h .. + 16 and 32 + 16 h .. + 16; of E2M1 steps 32 h .. + 32; and
+// supplies the scale of steps 32 h .. + 32.  Results: lane n + 32 h holds in register
+// i row 8 (i / 4) + 4 h + i % 4 of column n.  Row r of key block b is key
+// row_key(b, r), so that a lane's 32 scores are those of keys 32 h .. 32 h + 31 in
+// order: step k of the second product (16 keys) takes from lane half h keys 32 h +
+// 8 k .. + 8, so the weights need no exchange, and the value codes a lane of that
+// product takes are 32 consecutive ones.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mx.h"
+
+namespace ardit {
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Key of row r of key block b (32 rows each) of a tile.
+__device__ __forceinline__ int row_key(int b, int r) {
+  return 32 * ((r >> 2) & 1) + 16 * b + 4 * (r >> 3) + (r & 3);
+}
+
+// max / sum over lanes l and l ^ 32
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A query row's operands: hi and lo codes of 64 dims a step, and hi's scale bytes
+// (lo's are 4 less).
+template <int HD>
+struct Query {
+  i32x8 hi[HD / 64], lo[HD / 64];
+  int sc[HD / 64];
+};
+
+// 16 dims of a block (the lane 32 on has its other 16) into words w0 .. w0 + 3
+__device__ __forceinline__ void split_query(const uint4 (&raw)[2], i32x8& hi, i32x8& lo, int w0, int& sb) {
+  float f[16];
+  unpack8(raw[0], f);
+  unpack8(raw[1], f + 8);
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(f[i]));
+  m = pair_max(m);
+  // max / 2^e in [128, 256); at least 2^-113, so that lo's scale stays a byte
+  sb = max(static_cast<int>(__float_as_uint(m) >> 23) - 7, 14);
+  const float inv = __uint_as_float(static_cast<uint32_t>(254 - sb) << 23);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float a = f[4 * w] * inv, b = f[4 * w + 1] * inv, c = f[4 * w + 2] * inv, d = f[4 * w + 3] * inv;
+    int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    h = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, h, true);
+    const auto p = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), q = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+    int l = __builtin_amdgcn_cvt_pk_fp8_f32((a - p[0]) * 16.f, (b - p[1]) * 16.f, 0, false);
+    l = __builtin_amdgcn_cvt_pk_fp8_f32((c - q[0]) * 16.f, (d - q[1]) * 16.f, l, true);
+    hi[w0 + w] = h;
+    lo[w0 + w] = l;
+  }
+}
+
+// Query row at qp (its head's first dim); hh: lane / 32
+template <int HD>
+__device__ __forceinline__ void load_query(const bf16_t* qp, int hh, Query<HD>& q) {
+  uint4 raw[HD / 64][2][2];
+#pragma unroll
+  for (int ks = 0; ks < HD / 64; ++ks)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        raw[ks][b][i] = *reinterpret_cast<const uint4*>(qp + 64 * ks + 32 * b + 16 * hh + 8 * i);
+#pragma unroll
+  for (int ks = 0; ks < HD / 64; ++ks) {
+    int s0, s1;
+    split_query(raw[ks][0], q.hi[ks], q.lo[ks], 0, s0);
+    split_query(raw[ks][1], q.hi[ks], q.lo[ks], 4, s1);
+    q.sc[ks] = hh ? s1 : s0;
+  }
+}
+
+// S^T of 32 keys += their codes times the query's halves; sk: the key's scale bytes,
+// shifted by the lane's half: of the 64-dim step ks byte 2 ks.
+template <int HD, int BITS>
+__device__ __forceinline__ void score_block(const i32x8 (&k)[HD / 64], uint32_t sk, const Query<HD>& q, f32x16& s) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+  constexpr int FMT = BITS == 8 ? 0 : 4;
+#pragma unroll
+  for (int ks = 0; ks < HD / 64; ++ks) {
+    const int a = static_cast<int>((sk >> (16 * ks)) & 0xffu);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[ks], q.hi[ks], s, FMT, 0, 0, a, 0, q.sc[ks]);
+    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[ks], q.lo[ks], s, FMT, 0, 0, a, 0, q.sc[ks] - 4);
+  }
+}
+
+// ------------------------------------------------------------- few queries
+// A workgroup takes 32 rows of one (stream, head) and a cut of its key tiles, each of
+// its four waves every fourth tile; the waves meet in LDS.  Tiles are read straight
+// from memory (a wave's tile is its own), the next one's bytes while this one is
+// computed.  Cuts of one row tile leave partial results (unnormalised o, running
+// maximum, denominator) that a second kernel joins.
+constexpr int SM_BQ = 32;
+constexpr int SM_WAVES = 4;
+
+template <int HD, int BITS>
+struct TileBytes {
+  i32x8 k[2][HD / 64];
+  uint32_t ks[2];
+  u32x4 v[HD / 32][BITS / 4];
+  uint32_t vs[HD / 32];
+};
+
+template <int HD, int BITS>
+__device__ __forceinline__ void load_tile(const MxPages& p, size_t tile, int n, int hh, TileBytes<HD, BITS>& t) {
+  const uint8_t* kc = p.k + tile * mx_tile_bytes(HD, BITS);
+  const uint8_t* vc = p.v + tile * mx_tile_bytes(HD, BITS);
+  const uint8_t* ks = p.ks + tile * mx_scale_bytes(HD);
+  const uint8_t* vs = p.vs + tile * mx_scale_bytes(HD);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int key = row_key(b, n);
+    const uint8_t* row = kc + key * (HD * BITS / 8);
+#pragma unroll
+    for (int s = 0; s < HD / 64; ++s) {
+      if constexpr (BITS == 8) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * hh);
+        const u32x4 y = *reinterpret_cast<const u32x4*>(row + 64 * s + 32 + 16 * hh);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t.k[b][s][i] = static_cast<int>(x[i]);
+          t.k[b][s][4 + i] = static_cast<int>(y[i]);
+        }
+      } else {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(row + 32 * s + 16 * hh);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t.k[b][s][i] = static_cast<int>(x[i]);
+          t.k[b][s][4 + i] = 0;
+        }
+      }
+    }
+    if constexpr (HD == 128) t.ks[b] = *reinterpret_cast<const uint32_t*>(ks + 4 * key);
+    else t.ks[b] = *reinterpret_cast<const uint16_t*>(ks + 2 * key);
+  }
+#pragma unroll
+  for (int db = 0; db < HD / 32; ++db) {
+    const int dim = 32 * db + n;
+#pragma unroll
+    for (int i = 0; i < BITS / 4; ++i)
+      t.v[db][i] = *reinterpret_cast<const u32x4*>(vc + dim * (8 * BITS) + hh * (4 * BITS) + 16 * i);
+    t.vs[db] = vs[hh * HD + dim];
+  }
+}
+
+template <int HD, int BITS>
+__global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const MxSmallArgs a) {
+  constexpr int DB = HD / 32;
+  __shared__ __attribute__((aligned(16))) float part[SM_WAVES][SM_BQ][HD];
+  __shared__ float part_m[SM_WAVES][SM_BQ], part_l[SM_WAVES][SM_BQ];
+  const MxPages& p = a.p;
+  const int L = (static_cast<int>(blockIdx.x) % kNumXcd) * a.per_xcd + static_cast<int>(blockIdx.x) / kNumXcd;
+  if (L >= a.total_items) return;
+  int si = 0;
+  for (int i = 1; i < a.n_spans; ++i)
+    if (L >= a.s[i].item_begin) si = i;
+  const MxSpan S = a.s[si];
+  const int it = L - S.item_begin;
+  const int hp = it / S.n_qtiles, qt = it - hp * S.n_qtiles;
+  const int h = hp / S.pieces, piece = hp - h * S.pieces;
+  const int tb = S.tile0 + piece * S.per_piece, te = min(S.tile1, tb + S.per_piece);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+  const float c = a.scale_log2;
+
+  Query<HD> q;
+  load_query<HD>(a.q + static_cast<size_t>(S.q_off + min(qt * SM_BQ + n, S.q_len - 1)) * a.ld + h * HD, hh, q);
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  // (it starts finite, so that scores that all overflowed to -inf weigh nothing)
+  float m_run = kNoMax, l_run = 0.f;
+
+  // tile index and number of keys of tile t (a tile past the range: the last one's)
+  auto locate = [&](int t, int& keys) __attribute__((always_inline)) {
+    const int f = static_cast<int>(fdiv(static_cast<uint32_t>(t), p.fnt)), ti = t - f * p.nt;
+    keys = min(64, min(p.T, S.kv_len - f * p.T) - 64 * ti);
+    return mx_tile(p, mx_read_page(p, S.row, f), h, ti);
+  };
+  TileBytes<HD, BITS> now, next;
+  int keys = 0, keys_next = 0;
+  if (tb + wave < te) load_tile<HD, BITS>(p, locate(tb + wave, keys), n, hh, now);
+  for (int t = tb + wave; t < te; t += SM_WAVES) {
+    if (t + SM_WAVES < te) load_tile<HD, BITS>(p, locate(t + SM_WAVES, keys_next), n, hh, next);
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) score_block<HD, BITS>(now.k[b], now.ks[b] >> (8 * hh), q, s[b]);
+    if (keys < 64) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * hh + 16 * b + i >= keys) s[b][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    const float m_new = fmaxf(m_run, pair_max(mx) * c);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    bf16x8 pf[4];
+    const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 8 * (k & 1) + 2 * j;
+        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_new)),
+                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_new)));
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
+      }
+      pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const float sc = mx_scale(now.vs[db]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        u32x4 x;
+        if constexpr (BITS == 8) x = mx_decode8<8>(now.v[db][k >> 1][2 * (k & 1)], now.v[db][k >> 1][2 * (k & 1) + 1], sc);
+        else x = mx_decode8<4>(now.v[db][0][k], 0u, sc);
+        // values past the end are zero: whatever the page holds there would meet a zero weight
+        if (keys < 64) x = keep_first(x, keys - 32 * hh - 8 * k);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf[k], o[db], 0, 0, 0);
+      }
+    }
+    now = next;
+    keys = keys_next;
+  }
+
+  // the waves' results meet: o = sum_w 2^(m_w - M) o_w (a wave without tiles adds nothing)
+  const float l_tot = pair_sum(l_run);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {   // dims 32 db + 8 g + 4 hh .. + 4; 16-byte chunks XOR-swizzled by row
+      const int ch = 8 * db + 2 * g + hh;
+      *reinterpret_cast<float4*>(&part[wave][n][4 * (ch ^ (n & 15))]) =
+          make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+    }
+  if (hh == 0) {
+    part_m[wave][n] = m_run;
+    part_l[wave][n] = l_tot;
+  }
+  __syncthreads();
+  constexpr int TPR = HD / 4;
+  for (int i = tid; i < SM_BQ * TPR; i += 64 * SM_WAVES) {
+    const int row = i / TPR, c4 = i % TPR;
+    const int ql = qt * SM_BQ + row;
+    if (ql >= S.q_len) break;
+    float M = part_m[0][row];
+#pragma unroll
+    for (int w = 1; w < SM_WAVES; ++w) M = fmaxf(M, part_m[w][row]);
+    float l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < SM_WAVES; ++w) {
+      if (tb + w >= te) break;
+      const float wgt = __builtin_amdgcn_exp2f(part_m[w][row] - M);
+      const float4 x = *reinterpret_cast<const float4*>(&part[w][row][4 * (c4 ^ (row & 15))]);
+      l += wgt * part_l[w][row];
+      acc.x += wgt * x.x;
+      acc.y += wgt * x.y;
+      acc.z += wgt * x.z;
+      acc.w += wgt * x.w;
+    }
+    if (S.part_begin < 0) {
+      const float inv = 1.0f / l;
+      uint2 w;
+      w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+      w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>(a.o + static_cast<size_t>(S.q_off + ql) * a.ld + h * HD + 4 * c4) = w;
+    } else {
+      const size_t slot = S.part_begin + static_cast<size_t>(hp) * S.q_len + ql;
+      *reinterpret_cast<float4*>(a.part_o + slot * HD + 4 * c4) = acc;
+      if (c4 == 0) a.part_ml[slot] = make_float2(M, l);
+    }
+  }
+}
+
+// Joins the partial results of a row: those of its stream's cuts and, when the batch
+// shares a prefix, of the prefix's.
+template <int HD>
+__global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) {
+  constexpr int TPR = HD / 4, RPB = 256 / TPR;
+  const int i = static_cast<int>(blockIdx.x) * RPB + static_cast<int>(threadIdx.x) / TPR;   // head-major rows
+  const int c4 = threadIdx.x % TPR;
+  const int h = i / a.rows, r = i - h * a.rows;
+  if (h >= a.p.H) return;
+  int si = a.shared;
+  for (int j = a.shared + 1; j < a.n_spans; ++j)
+    if (r >= a.s[j].q_off) si = j;
+  const MxSpan& S = a.s[si];
+  if (S.part_begin < 0) return;   // written whole
+  const MxSpan& P = a.s[0];
+  const int own = S.pieces, all = own + (a.shared ? P.pieces : 0);
+  auto slot = [&](int j) {
+    return j < own ? S.part_begin + (static_cast<size_t>(h) * own + j) * S.q_len + (r - S.q_off)
+                   : P.part_begin + (static_cast<size_t>(h) * P.pieces + j - own) * P.q_len + r;
+  };
+  float M = kNoMax;
+  for (int j = 0; j < all; ++j) M = fmaxf(M, a.part_ml[slot(j)].x);
+  float l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j = 0; j < all; ++j) {
+    const size_t at = slot(j);
+    const float2 ml = a.part_ml[at];
+    const float wgt = __builtin_amdgcn_exp2f(ml.x - M);
+    const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * HD + 4 * c4);
+    l += wgt * ml.y;
+    acc.x += wgt * x.x;
+    acc.y += wgt * x.y;
+    acc.z += wgt * x.z;
+    acc.w += wgt * x.w;
+  }
+  const float inv = 1.0f / l;
+  uint2 w;
+  w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+  w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+  *reinterpret_cast<uint2*>(a.o + static_cast<size_t>(r) * a.ld + h * HD + 4 * c4) = w;
+}
+
+template <int HD, int BITS>
+hipError_t launch_small(hipStream_t st, const MxSmallArgs& a, bool join) {
+  hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
+  if (join) {
+    constexpr int RPB = 256 / (HD / 4);
+    hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + RPB - 1) / RPB), dim3(256), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
+
+// Cuts the spans' key tiles so that the workgroups fill one round of the GPU and the
+// partial rows fit max_rows.  True when some span leaves partial results.
+bool plan_small(MxSmallArgs& a, int64_t max_rows) {
+  int64_t cost = 0;
+  int most = 0;
+  for (int i = 0; i < a.n_spans; ++i) {
+    MxSpan& s = a.s[i];
+    s.n_qtiles = (s.q_len + SM_BQ - 1) / SM_BQ;
+    cost += static_cast<int64_t>(s.n_qtiles) * a.p.H * (s.tile1 - s.tile0);
+    most = std::max(most, s.tile1 - s.tile0);
+  }
+  auto fits = [&](int w) {
+    int64_t items = 0, rows = 0;
+    for (int i = 0; i < a.n_spans; ++i) {
+      const MxSpan& s = a.s[i];
+      const int64_t pieces = std::max(1, (s.tile1 - s.tile0 + w - 1) / w);
+      items += s.n_qtiles * pieces * a.p.H;
+      if (pieces > 1 || a.shared) rows += s.q_len * pieces * a.p.H;
+    }
+    return items <= kSmallRound && rows <= max_rows;
+  };
+  int W = static_cast<int>(std::max<int64_t>(SM_WAVES, (cost + kSmallRound - 1) / kSmallRound));
+  while (W < most && !fits(W)) W += std::max(1, W / 16);
+  W = std::min(W, std::max(most, 1));
+  bool join = false;
+  int64_t items = 0, rows = 0;
+  for (int i = 0; i < a.n_spans; ++i) {
+    MxSpan& s = a.s[i];
+    const int tiles = s.tile1 - s.tile0;
+    s.pieces = std::max(1, (tiles + W - 1) / W);
+    s.per_piece = (tiles + s.pieces - 1) / s.pieces;
+    s.item_begin = static_cast<int32_t>(items);
+    items += static_cast<int64_t>(s.n_qtiles) * a.p.H * s.pieces;
+    s.part_begin = -1;
+    if (s.pieces > 1 || a.shared) {
+      s.part_begin = static_cast<int32_t>(rows);
+      rows += static_cast<int64_t>(a.p.H) * s.pieces * s.q_len;
+      join = true;
+    }
+  }
+  a.total_items = static_cast<int32_t>(items);
+  a.per_xcd = (a.total_items + kNumXcd - 1) / kNumXcd;
+  return join;
+}
+
+}  // namespace
+
+hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
+                               const RowStreams& rs, int shared, float* part) {
+  MxSmallArgs a;
+  a.p = p;
+  a.q = q;
+  a.o = o;
+  a.ld = p.H * p.hd;
+  a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.hd)));
+  a.rows = 0;
+  int row_tiles = 0, first = -1;
+  for (int i = 0; i < rs.n; ++i) {
+    a.rows += rs.s[i].len;
+    row_tiles += (rs.s[i].len + SM_BQ - 1) / SM_BQ;
+    if (first < 0 && rs.s[i].len > 0) first = i;
+  }
+  if (a.rows == 0) return hipSuccess;
+  const int64_t max_rows = static_cast<int64_t>(attention_split_bytes(p.hd) / (sizeof(float) * (p.hd + 2)));
+  a.part_o = part;
+  a.part_ml = reinterpret_cast<float2*>(part + max_rows * p.hd);
+  // The prefix is walked once for all rows where that makes fewer row tiles.
+  a.shared = shared > 0 && (a.rows + SM_BQ - 1) / SM_BQ < row_tiles &&
+             static_cast<int64_t>(2) * p.H * a.rows <= max_rows;
+  const int32_t tile0 = a.shared ? shared * p.nt : 0;
+  a.n_spans = 0;
+  if (a.shared) {
+    MxSpan& s = a.s[a.n_spans++];
+    s.q_off = 0;
+    s.q_len = a.rows;
+    s.kv_len = shared * p.T;
+    s.row = first;
+    s.tile0 = 0;
+    s.tile1 = tile0;
+  }
+  for (int i = 0; i < rs.n; ++i) {
+    if (rs.s[i].len == 0) continue;
+    MxSpan& s = a.s[a.n_spans++];
+    s.q_off = rs.s[i].row_begin;
+    s.q_len = rs.s[i].len;
+    s.kv_len = rs.s[i].cache_len + rs.s[i].len;
+    s.row = i;
+    s.tile0 = tile0;
+    s.tile1 = static_cast<int32_t>(mx_tiles(s.kv_len, p.T, p.nt));
+  }
+  const bool join = plan_small(a, max_rows);
+  if (p.hd == 128) return p.bits == 8 ? launch_small<128, 8>(st, a, join) : launch_small<128, 4>(st, a, join);
+  return p.bits == 8 ? launch_small<64, 8>(st, a, join) : launch_small<64, 4>(st, a, join);
+}
+
+}  // namespace ardit

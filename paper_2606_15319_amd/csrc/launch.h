@@ -231,6 +231,67 @@ struct SamplerArgs {
 hipError_t launch_sampler(hipStream_t st, const bf16_t* x, const bf16_t* v, const bf16_t* eps,
                           bf16_t* out, const SamplerArgs& a);
 
+// ------------------------------------------- microscaled key/value pages
+// Codes of 8 (E4M3) or 4 (E2M1) bits in blocks of 32 with a power-of-two scale
+// each, in tiles of 64 keys of one page: T64 = 64 nt keys a page, of which T
+// exist.  ardit.h gives the layout.
+struct MxPages {
+  uint8_t *k, *ks, *v, *vs;
+  const int32_t* page_table;
+  int32_t max_frames, n_pages;
+  int32_t T, nt;         // keys and tiles of a page
+  int32_t H, hd, bits;
+  FastDiv fT, fnt;
+};
+
+// QK-norm + RoPE of the rows of qkv (columns q | k | v): q_out, and the chunk's
+// keys and values quantised into the pages.  Whole frames per stream.
+hipError_t launch_kv_append_mx(hipStream_t st, const bf16_t* qkv, int N, const RopeGeom& g,
+                               const bf16_t* g_q, const bf16_t* g_k, bf16_t* q_out,
+                               const MxPages& p, const RowStreams& rs);
+
+// Logical tokens [cache_len, cache_len + len) of each stream of rs (cache_len a
+// multiple of T) from the pages p to the bf16 pages k / v through their own table.
+hipError_t launch_kv_read_mx(hipStream_t st, const MxPages& p, bf16_t* k_pages, bf16_t* v_pages,
+                             const int32_t* page_table, int max_frames, int n_pages,
+                             const RowStreams& rs);
+
+// One stream's part of an attention over microscaled pages: rows of the packed
+// queries against key tiles [tile0, tile1) of a page table row (tile t: tile t %
+// nt of frame t / nt).
+struct MxSpan {
+  int32_t q_off, q_len;
+  int32_t kv_len;        // keys [0, kv_len)
+  int32_t row;           // row of the page table
+  int32_t tile0, tile1;
+  int32_t n_qtiles, pieces, per_piece;   // row tiles; cuts of the key tiles, and tiles of a cut
+  int32_t item_begin;    // first workgroup
+  int32_t part_begin;    // first partial row; -1: the output is written whole
+};
+struct MxSmallArgs {
+  MxPages p;
+  const bf16_t* q;
+  bf16_t* o;
+  int32_t ld;
+  float scale_log2;      // log2(e) / sqrt(d)
+  int32_t n_spans, shared;   // shared: span 0 is the common prefix, of all rows
+  int32_t total_items, per_xcd;
+  int32_t rows;          // rows of the packed queries
+  float* part_o;         // [partial rows][hd]
+  float2* part_ml;       // [partial rows] running max, denominator
+  MxSpan s[kMaxStreams + 1];
+};
+static_assert(sizeof(MxSmallArgs) <= 4096, "arguments must fit the kernel-argument buffer");
+// Key tiles of kv_len keys in pages of T keys.
+inline int64_t mx_tiles(int64_t kv_len, int64_t T, int64_t nt) {
+  return kv_len / T * nt + (kv_len % T + kAttnKTile - 1) / kAttnKTile;
+}
+// Plans and launches the attention of a batch over microscaled pages.  rs: rows
+// of each stream and its keys (kv_len = cache_len + len).  shared: frames of the
+// common prefix.  part: attention_split_bytes of scratch.
+hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
+                               const RowStreams& rs, int shared, float* part);
+
 // ------------------------------------------------------ measurement
 // flops one wave performs per iteration of the MFMA peak kernel
 double micro_mfma_flops_per_wave_iter(int dtype);
