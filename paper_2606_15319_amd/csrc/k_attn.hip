@@ -1209,7 +1209,7 @@ int64_t split_end(const AttnStream* s, int n, int split_tiles, int64_t tails, in
 
 }  // namespace
 
-void plan_attention(AttnArgs& a, int head_dim, float* split_ws) {
+void plan_attention(AttnArgs& a, int head_dim, float* split_ws, bool small) {
   // order streams by decreasing key count so the longest items start first
   AttnStream tmp[kMaxStreams];
   int n = 0;
@@ -1263,7 +1263,7 @@ void plan_attention(AttnArgs& a, int head_dim, float* split_ws) {
       wgs += static_cast<int64_t>((tmp[i].q_len + SM_BQ - 1) / SM_BQ) * a.H;
       most = tmp[i].n_tiles > most ? tmp[i].n_tiles : most;
     }
-    if (items > 0 && wgs <= kAttnSplitBlocks && most <= small_tiles(head_dim)) {
+    if (small && items > 0 && wgs <= kAttnSplitBlocks && most <= small_tiles(head_dim)) {
       a.small = 1;
       a.total_items = static_cast<int32_t>(wgs);
       a.per_xcd = (a.total_items + kNumXcd - 1) / kNumXcd;
@@ -1340,6 +1340,15 @@ void plan_attention(AttnArgs& a, int head_dim, float* split_ws) {
   }
   for (int i = 0; i < n; ++i) a.s[i] = tmp[i];
   if (!a.split_blocks) balance_items_over_xcds(a, false);
+}
+
+hipError_t launch_attention_merge(hipStream_t st, const AttnArgs& a, int head_dim) {
+  const int items = a.total_items - a.item0;
+  if (head_dim == 128)
+    hipLaunchKernelGGL((attn_merge_kernel<128>), dim3(items * (BQ / 8)), dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((attn_merge_kernel<64>), dim3(items * (BQ / 16)), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 constexpr size_t kAloneLds = 20 * 1024;   // 64 + 20 KB: one workgroup in a CU's 160 KB

@@ -25,8 +25,10 @@
 // 8 k .. + 8, so the weights need no exchange, and the value codes a lane of that
 // product takes are 32 consecutive ones.
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mx.h"
 
@@ -367,6 +369,422 @@ __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) 
   *reinterpret_cast<uint2*>(a.o + static_cast<size_t>(r) * a.ld + h * HD + 4 * c4) = w;
 }
 
+// ------------------------------------------------------------ whole chunks
+// Items of 256 queries of one (stream, head), eight waves of 32 rows; key tiles are
+// shared through LDS.  AttnArgs is planned as for the bf16 attention, with a
+// stream's tiles counted page by page; base_off holds its number of keys.
+struct MxLargeArgs {
+  AttnArgs a;
+  MxPages p;
+};
+static_assert(sizeof(MxLargeArgs) <= 4096, "arguments must fit the kernel-argument buffer");
+
+constexpr int BQ = 256;
+constexpr int NTHR = 512;
+constexpr int NSLOT = 4;     // tiles of codes in LDS
+
+// 16-byte chunk c of an LDS row of ROWB bytes sits at chunk c ^ swz(r): 16 rows then
+// cover every bank for a fixed c.
+template <int ROWB>
+__device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 16 - 1); }
+
+template <int HD, int BITS>
+struct LargeLds {
+  uint8_t k[NSLOT][mx_tile_bytes(HD, BITS)];      // row R = 32 b + r: key row_key(b, r)
+  uint8_t v[NSLOT][mx_tile_bytes(HD, BITS)];      // as in the page
+  bf16_t vb[2][64 * HD];                          // [dim][64 keys]
+  uint8_t ks[NSLOT][mx_scale_bytes(HD)];
+  uint8_t vs[NSLOT][mx_scale_bytes(HD)];
+};
+
+// Runs key tiles [tb, te) of item (S, head h, query tile qt), then writes the
+// normalised output (slot < 0) or partial results into slot `slot`.
+//
+// The two waves of a SIMD run half a tile apart, as in the bf16 attention: a position's
+// work is an MFMA phase (O += V P of the position before, S = K Q) and a VALU phase
+// (softmax, requests for tiles to come), one barrier a position, group 0 before its
+// MFMA phase and group 1 before its VALU phase.  Interval t (after barrier t) reads
+// the keys of position t, turns its value codes into bf16 (slot t % 2, each thread
+// HD / 8 of them) and reads the bf16 values of position t - 1; it requests the codes
+// and scales of position t + 3, whose slots were last read in interval t - 1.
+template <int HD, int BITS>
+__device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, const AttnStream& S, int h, int qt,
+                                         int tb, int te, LargeLds<HD, BITS>& lds, int64_t slot) {
+  constexpr int KS = HD / 64, DB = HD / 32;
+  constexpr int TB = mx_tile_bytes(HD, BITS), SB = mx_scale_bytes(HD);
+  constexpr int NL = TB / 1024;            // 1 KB loads of a tile of keys, and of values
+  constexpr int KROW = HD * BITS / 8;      // bytes of a key
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n32 = lane & 31, hh = lane >> 5;
+  const int grp = wave >> 2;
+  const int n = te - tb;
+  const float c = a.scale_log2;
+  const int kv_len = S.base_off;
+
+  Query<HD> q;
+  load_query<HD>(a.q + static_cast<size_t>(S.q_off + min(qt * BQ + wave * 32 + n32, S.q_len - 1)) * a.ldq + h * HD,
+                 hh, q);
+
+  // ---- staging by direct loads.  Eight loads a tile: every wave one of keys and one of
+  // values; four: waves 0-3 keys, 4-7 values; two: waves 0, 1 and 4, 5.
+  constexpr bool BOTH = NL == 8;
+  const bool loads_k = BOTH || wave < NL, loads_v = BOTH || (wave >= 4 && wave - 4 < NL);
+  const int piece = BOTH ? wave : (wave & 3);
+  const int ks_wave = NL == 2 ? 2 : 0, vs_wave = NL == 2 ? 6 : (BOTH ? 1 : 4);
+  const int kR = piece * (1024 / KROW) + lane / (KROW / 16);
+  const uint32_t k_off = static_cast<uint32_t>(row_key((kR >> 5) & 1, kR & 31) * KROW +
+                                               (((lane % (KROW / 16)) ^ swz<KROW>(kR)) << 4));
+  const uint32_t v_off = static_cast<uint32_t>(piece * 1024 + lane * 16);
+  const uint32_t s_off = static_cast<uint32_t>(lane * 4);
+  const uint32_t lds_k = lds_address(lds.k) + piece * 1024u, lds_v = lds_address(lds.v) + piece * 1024u;
+  const uint32_t lds_ks = lds_address(lds.ks), lds_vs = lds_address(lds.vs);
+
+  const int last_frame = static_cast<int>(fdiv(static_cast<uint32_t>(kv_len - 1), p.fT));
+  const int32_t* pt = p.page_table + static_cast<size_t>(S.stream) * p.max_frames;
+  // lane i: page of frame f0 + i, clamped into the pool
+  auto page_window = [&](int f0) __attribute__((always_inline)) {
+    return min(max(pt[min(f0 + lane, last_frame)], 0), p.n_pages - 1);
+  };
+  int fr = static_cast<int>(fdiv(static_cast<uint32_t>(tb), p.fnt));   // frame and tile requested next
+  int ti = tb - fr * p.nt;
+  int pw0 = fr, pw = page_window(fr);
+  size_t tile = mx_tile(p, __builtin_amdgcn_readlane(pw, 0), h, ti);
+  // requests position u, the one after those requested (u < n)
+  auto stage = [&](int u) __attribute__((always_inline)) {
+    const uint32_t sl = static_cast<uint32_t>(u % NSLOT);
+    const char* kc = reinterpret_cast<const char*>(p.k) + tile * TB;
+    const char* vc = reinterpret_cast<const char*>(p.v) + tile * TB;
+    if (loads_k) lds_dma16(kc, k_off, lds_k + sl * TB);
+    if (loads_v) lds_dma16(vc, v_off, lds_v + sl * TB);
+    if (wave == ks_wave && lane < SB / 4)
+      lds_dma4(reinterpret_cast<const char*>(p.ks) + tile * SB, s_off, lds_ks + sl * SB);
+    if (wave == vs_wave && lane < SB / 4)
+      lds_dma4(reinterpret_cast<const char*>(p.vs) + tile * SB, s_off, lds_vs + sl * SB);
+    ++tile;
+    if (++ti == p.nt) {
+      ti = 0;
+      ++fr;
+      if (fr - pw0 >= 64) {
+        pw0 = fr;
+        pw = page_window(fr);
+        asm volatile("" : "+v"(pw));   // waited for here, so no later wait has to
+      }
+      if (u + 1 < n) tile = mx_tile(p, __builtin_amdgcn_readlane(pw, fr - pw0), h, 0);
+    }
+  };
+  const int per_pair = (loads_k ? 1 : 0) + (loads_v ? 1 : 0) + (wave == ks_wave ? 1 : 0) + (wave == vs_wave ? 1 : 0);
+  // all but the last P positions requested by this wave have landed
+  auto wait_pairs = [&](auto pairs_c) __attribute__((always_inline)) {
+    constexpr int P = decltype(pairs_c)::value;
+    if (per_pair == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * P) : "memory");
+    else if (per_pair == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * P) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P) : "memory");
+  };
+  const std::integral_constant<int, 0> w0;
+  const std::integral_constant<int, 2> w2;
+  const std::integral_constant<int, 3> w3;
+  // keys of position t's tile
+  auto keys_of = [&](int t) __attribute__((always_inline)) {
+    const int f = static_cast<int>(fdiv(static_cast<uint32_t>(tb + t), p.fnt));
+    return min(64, min(p.T, kv_len - f * p.T) - 64 * (tb + t - f * p.nt));
+  };
+
+  f32x16 o[DB], s[2];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m_run = kNoMax, l_run = 0.f;
+  bf16x8 pf[4];
+
+  // value codes of position t to bf16: this thread HD / 8 keys of one dim
+  auto convert = [&](int t, int keys) __attribute__((always_inline)) {
+    constexpr int E = HD / 8;
+    const int dim = tid / (64 / E), k0 = E * (tid % (64 / E));
+    const uint8_t* src = lds.v[t % NSLOT] + tid * (E * BITS / 8);
+    const float sc = mx_scale(lds.vs[t % NSLOT][(k0 >> 5) * HD + dim]);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if constexpr (E * BITS == 128) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(src);
+      w[0] = x[0]; w[1] = x[1]; w[2] = x[2]; w[3] = x[3];
+    } else if constexpr (E * BITS == 64) {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      w[0] = x.x; w[1] = x.y;
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(src);
+    }
+    bf16_t* dst = lds.vb[t & 1] + dim * 64;
+#pragma unroll
+    for (int i = 0; i < E / 8; ++i) {
+      u32x4 x = BITS == 8 ? mx_decode8<BITS>(w[2 * i], w[2 * i + 1], sc) : mx_decode8<BITS>(w[i], 0u, sc);
+      if (keys < 64) x = keep_first(x, keys - k0 - 8 * i);
+      *reinterpret_cast<u32x4*>(dst + 8 * ((k0 / 8 + i) ^ swz<128>(dim))) = x;
+    }
+  };
+
+  auto mfma_phase = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
+    constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
+    __builtin_amdgcn_s_setprio(1);
+    if constexpr (PV) {
+      const bf16_t* tv = lds.vb[(t - 1) & 1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const int dim = 32 * db + n32;
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(tv + dim * 64 + 8 * ((4 * hh + k) ^ swz<128>(n32)));
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[db], 0, 0, 0);
+        }
+    }
+    if constexpr (QK) {
+      const uint8_t* tk = lds.k[t % NSLOT];
+      i32x8 kf[2][KS];
+      uint32_t sk[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int R = 32 * b + n32, key = row_key(b, n32);
+        if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(lds.ks[t % NSLOT] + 4 * key);
+        else sk[b] = *reinterpret_cast<const uint16_t*>(lds.ks[t % NSLOT] + 2 * key);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (BITS == 8) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((4 * ks + hh) ^ swz<KROW>(R)) << 4));
+            const u32x4 y = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((4 * ks + 2 + hh) ^ swz<KROW>(R)) << 4));
+            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
+                              static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
+          } else {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((2 * ks + hh) ^ swz<KROW>(R)) << 4));
+            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]), 0, 0, 0, 0};
+          }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) score_block<HD, BITS>(kf[b], sk[b] >> (8 * hh), q, s[b]);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (HD == 128) __builtin_amdgcn_sched_barrier(0);
+  };
+
+  auto softmax = [&](int keys) __attribute__((always_inline)) {
+    if (keys < 64) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * hh + 16 * b + i >= keys) s[b][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = pair_max(mx) * c;
+    // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
+    // 2^8), so that o is seldom rescaled
+    if (__any(mx > m_run + 8.0f)) {
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+    const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 8 * (k & 1) + 2 * j;
+        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run)),
+                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_run)));
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
+      }
+      pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+    }
+    if constexpr (HD == 128)
+      asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]), "+v"(l_run));
+  };
+  const std::true_type yes;
+  const std::false_type no;
+
+  // ---- prologue: the positions ahead of the group's first VALU phase
+#pragma unroll 1
+  for (int u = 0; u < 3 + grp; ++u)
+    if (u < n) stage(u);
+  if (3 + grp > n) wait_pairs(w0);
+  else if (grp == 0) wait_pairs(w2);
+  else wait_pairs(w3);
+  __syncthreads();
+  auto wait_next = [&](int u) __attribute__((always_inline)) {   // u: the last position requested
+    if (u < n) wait_pairs(w2);
+    else wait_pairs(w0);
+  };
+  const bool rows = qt * BQ + wave * 32 < S.q_len;   // else: the wave only stages and converts
+  if (grp == 0) {
+    if (rows) mfma_phase(0, no, yes);
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      const int keys = keys_of(t);
+      if (t + 3 < n) stage(t + 3);
+      if (rows) softmax(keys);
+      convert(t, keys);
+      wait_next(t + 3);
+      __syncthreads();
+      if (rows) {
+        if (t + 1 < n) mfma_phase(t + 1, yes, yes);
+        else mfma_phase(n, yes, no);
+      }
+    }
+  } else {
+    convert(0, keys_of(0));
+    if (rows) mfma_phase(0, no, yes);
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      wait_next(t + 3);
+      __syncthreads();
+      if (t + 4 < n) stage(t + 4);
+      if (rows) softmax(keys_of(t));
+      if (t + 1 < n) {
+        convert(t + 1, keys_of(t + 1));
+        if (rows) mfma_phase(t + 1, yes, yes);
+      } else if (rows) {
+        mfma_phase(n, yes, no);
+      }
+    }
+  }
+
+  // ---- lane n32 + 32 hh holds dims 32 db + 8 g + 4 hh .. + 4 of its query
+  const float l_tot = pair_sum(l_run);
+  const int row = wave * 32 + n32, ql = qt * BQ + row;
+  if (slot < 0) {
+    const float inv = 1.0f / l_tot;
+    if (ql < S.q_len) {
+      bf16_t* op = a.o + static_cast<size_t>(S.q_off + ql) * a.ldo + h * HD;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint2 w;
+          w.x = pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
+          w.y = pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+          *reinterpret_cast<uint2*>(op + 32 * db + 8 * g + 4 * hh) = w;
+        }
+    }
+  } else {
+    float* po = a.part_o + (static_cast<size_t>(slot) * BQ + row) * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(po + 32 * db + 8 * g + 4 * hh) =
+            make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+    if (hh == 0) {
+      a.part_ml[static_cast<size_t>(slot) * 2 * BQ + row] = m_run;
+      a.part_ml[static_cast<size_t>(slot) * 2 * BQ + BQ + row] = l_tot;
+    }
+    __syncthreads();   // a following range reuses the tiles
+  }
+}
+
+__device__ __forceinline__ int item_stream(const AttnArgs& a, int item) {
+  int si = 0;
+  for (int i = 1; i < a.n_streams; ++i)
+    if (item >= a.s[i].item_begin) si = i;
+  return si;
+}
+
+// One workgroup per item, each XCD a contiguous range of them.
+template <int HD, int BITS>
+__global__ __launch_bounds__(NTHR, HD == 64 ? 4 : 1) void attn_mx_kernel(const MxLargeArgs x) {
+  __shared__ __attribute__((aligned(1024))) LargeLds<HD, BITS> lds;
+  const AttnArgs& a = x.a;
+  const int xcd = blockIdx.x % kNumXcd;
+  const int L = a.xcd_begin[xcd] + blockIdx.x / kNumXcd;
+  if (L >= a.xcd_begin[xcd + 1]) return;
+  const AttnStream S = a.s[item_stream(a, L)];
+  const int it = L - S.item_begin, h = it / S.n_qtiles;
+  mx_range<HD, BITS>(a, x.p, S, h, it - h * S.n_qtiles, 0, S.n_tiles, lds, -1);
+}
+
+// The split schedule of plan_attention: main parts of the items from item0 on, then
+// equal ranges of their concatenated tails (slots as attn_merge_kernel reads them).
+template <int HD, int BITS>
+__global__ __launch_bounds__(NTHR, 1) void attn_mx_split_kernel(const MxLargeArgs x) {
+  __shared__ __attribute__((aligned(1024))) LargeLds<HD, BITS> lds;
+  const AttnArgs& a = x.a;
+  const int xcd = blockIdx.x % kNumXcd, j = blockIdx.x / kNumXcd;
+  const int items = a.total_items - a.item0;
+  const int ipx = items / kNumXcd, irem = items % kNumXcd;
+  const int nx = ipx + (xcd < irem ? 1 : 0), pre = xcd * ipx + min(xcd, irem);
+  if (j < nx) {
+    const int gi = a.item0 + pre + j;
+    const AttnStream S = a.s[item_stream(a, gi)];
+    const int item = gi - S.item_begin, h = item / S.n_qtiles;
+    mx_range<HD, BITS>(a, x.p, S, h, item - h * S.n_qtiles, 0, S.main_tiles, lds,
+                       S.main_tiles == S.n_tiles ? -1 : gi - a.item0);
+    return;
+  }
+  const int r = a.per_xcd * xcd + j - (pre + nx);
+  if (r >= a.split_blocks - items) return;
+  int pos = r * a.split_tiles;
+  const int end = min(pos + a.split_tiles, a.total_tiles);
+  while (pos < end) {
+    int si = 0;
+    for (int i = 1; i < a.n_streams; ++i)
+      if (pos >= a.s[i].tail_begin) si = i;
+    const AttnStream S = a.s[si];
+    const int tl = S.n_tiles - S.main_tiles, rel = pos - S.tail_begin;
+    const int item = max(0, a.item0 - S.item_begin) + rel / tl;
+    const int tb = S.main_tiles + rel % tl, te = min(S.n_tiles, tb + (end - pos));
+    pos += te - tb;
+    const int h = item / S.n_qtiles;
+    mx_range<HD, BITS>(a, x.p, S, h, item - h * S.n_qtiles, tb, te, lds,
+                       static_cast<int64_t>(items) + S.item_begin + item - a.item0 + r);
+  }
+}
+
+template <int HD, int BITS>
+hipError_t launch_large(hipStream_t st, const MxLargeArgs& x) {
+  const AttnArgs& a = x.a;
+  if (a.split_blocks) {
+    if (a.item0 > 0) hipLaunchKernelGGL((attn_mx_kernel<HD, BITS>), dim3(a.item0), dim3(NTHR), 0, st, x);
+    hipLaunchKernelGGL((attn_mx_split_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(NTHR), 0, st, x);
+    return launch_attention_merge(st, a, HD);
+  }
+  hipLaunchKernelGGL((attn_mx_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(NTHR), 0, st, x);
+  return hipGetLastError();
+}
+
+// Whole-chunk attention of all streams.
+hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o, const RowStreams& rs,
+                     float* part) {
+  MxLargeArgs x;
+  memset(&x, 0, sizeof(x));
+  x.p = p;
+  AttnArgs& a = x.a;
+  a.q = q;
+  a.o = o;
+  a.ldq = a.ldo = p.H * p.hd;
+  a.H = p.H;
+  a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.hd)));
+  a.n_streams = rs.n;
+  for (int i = 0; i < rs.n; ++i) {
+    AttnStream& s = a.s[i];
+    s.q_off = rs.s[i].row_begin;
+    s.q_len = rs.s[i].len;
+    s.stream = i;
+    s.base_off = rs.s[i].cache_len + rs.s[i].len;
+    s.kv_len = static_cast<int32_t>(kAttnKTile * mx_tiles(s.base_off, p.T, p.nt));   // as planned: whole tiles
+  }
+  plan_attention(a, p.hd, part, false);
+  if (p.hd == 128) return p.bits == 8 ? launch_large<128, 8>(st, x) : launch_large<128, 4>(st, x);
+  return p.bits == 8 ? launch_large<64, 8>(st, x) : launch_large<64, 4>(st, x);
+}
+
 template <int HD, int BITS>
 hipError_t launch_small(hipStream_t st, const MxSmallArgs& a, bool join) {
   hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
@@ -442,6 +860,7 @@ hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q
     if (first < 0 && rs.s[i].len > 0) first = i;
   }
   if (a.rows == 0) return hipSuccess;
+  if (a.rows > 32 * row_tiles / 2 && row_tiles * p.H > 128) return run_large(st, p, q, o, rs, part);
   const int64_t max_rows = static_cast<int64_t>(attention_split_bytes(p.hd) / (sizeof(float) * (p.hd + 2)));
   a.part_o = part;
   a.part_ml = reinterpret_cast<float2*>(part + max_rows * p.hd);

@@ -113,7 +113,10 @@ size_t attention_split_bytes(int head_dim);
 // Fills the schedule fields from the streams' lengths, ordering streams by
 // decreasing key count.  split_ws (attention_split_bytes, or null to never
 // split) receives the partial results when the items are cut between workgroups.
-void plan_attention(AttnArgs& a, int head_dim, float* split_ws);
+// small: calls of few queries over few keys may take 32-query workgroups.
+void plan_attention(AttnArgs& a, int head_dim, float* split_ws, bool small = true);
+// Joins the partial results of a split schedule's items.
+hipError_t launch_attention_merge(hipStream_t st, const AttnArgs& a, int head_dim);
 hipError_t launch_attention(hipStream_t st, const AttnArgs& a, int head_dim, bool paged);
 
 // ---------------------------------------------------------- FP8 attention
