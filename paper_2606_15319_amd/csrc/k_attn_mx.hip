@@ -107,18 +107,30 @@ __device__ __forceinline__ void load_query(const bf16_t* qp, int hh, Query<HD>& 
   }
 }
 
-// S^T of 32 keys += their codes times the query's halves; sk: the key's scale bytes,
-// shifted by the lane's half: of the 64-dim step ks byte 2 ks.
+// S^T of a tile's two 32-key blocks; sk: each key's scale bytes, shifted by the lane's
+// half, so that byte 2 ks is that of the 64-dim step ks.
 template <int HD, int BITS>
-__device__ __forceinline__ void score_block(const i32x8 (&k)[HD / 64], uint32_t sk, const Query<HD>& q, f32x16& s) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+__device__ __forceinline__ void scores(const i32x8 (&k)[2][HD / 64], const uint32_t (&sk)[2], const Query<HD>& q,
+                                       f32x16 (&s)[2]) {
   constexpr int FMT = BITS == 8 ? 0 : 4;
 #pragma unroll
-  for (int ks = 0; ks < HD / 64; ++ks) {
-    const int a = static_cast<int>((sk >> (16 * ks)) & 0xffu);
-    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[ks], q.hi[ks], s, FMT, 0, 0, a, 0, q.sc[ks]);
-    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[ks], q.lo[ks], s, FMT, 0, 0, a, 0, q.sc[ks] - 4);
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+  // (the scale operand's byte 2 ks: an immediate of the instruction)
+#pragma unroll
+  for (int lo = 0; lo < 2; ++lo)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][0], lo ? q.lo[0] : q.hi[0], s[b], FMT, 0, 0,
+                                                              static_cast<int>(sk[b]), 0, q.sc[0] - 4 * lo);
+  if constexpr (HD == 128) {
+#pragma unroll
+    for (int lo = 0; lo < 2; ++lo)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][1], lo ? q.lo[1] : q.hi[1], s[b], FMT, 0, 2,
+                                                                static_cast<int>(sk[b]), 0, q.sc[1] - 4 * lo);
   }
 }
 
@@ -224,14 +236,14 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   for (int t = tb + wave; t < te; t += SM_WAVES) {
     if (t + SM_WAVES < te) load_tile<HD, BITS>(p, locate(t + SM_WAVES, keys_next), n, hh, next);
     f32x16 s[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) score_block<HD, BITS>(now.k[b], now.ks[b] >> (8 * hh), q, s[b]);
+    const uint32_t sk[2] = {now.ks[0] >> (8 * hh), now.ks[1] >> (8 * hh)};
+    scores<HD, BITS>(now.k, sk, q, s);
     if (keys < 64) {
+      const int left = keys - 32 * hh;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * hh + 16 * b + i >= keys) s[b][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) s[b][i] = 16 * b + i < left ? s[b][i] : -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -381,15 +393,22 @@ static_assert(sizeof(MxLargeArgs) <= 4096, "arguments must fit the kernel-argume
 
 constexpr int BQ = 256;
 constexpr int NTHR = 512;
-constexpr int NSLOT = 4;     // tiles of codes in LDS
+
 
 // 16-byte chunk c of an LDS row of ROWB bytes sits at chunk c ^ swz(r): 16 rows then
 // cover every bank for a fixed c.
 template <int ROWB>
 __device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 16 - 1); }
 
+// Tiles requested ahead of the one computed.  At d = 64 key fragments are read before
+// the barrier that their products follow (they have to have landed one barrier sooner):
+// 4680 queries over 14040 keys, 20 heads of 64, 522 us for 545; at d = 128 486 for 475
+// (12 heads).
+constexpr int ahead(int hd) { return hd == 64 ? 4 : 3; }
+
 template <int HD, int BITS>
 struct LargeLds {
+  static constexpr int NSLOT = ahead(HD) + 1;     // tiles of codes
   uint8_t k[NSLOT][mx_tile_bytes(HD, BITS)];      // row R = 32 b + r: key row_key(b, r)
   uint8_t v[NSLOT][mx_tile_bytes(HD, BITS)];      // as in the page
   bf16_t vb[2][64 * HD];                          // [dim][64 keys]
@@ -414,6 +433,8 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
   constexpr int TB = mx_tile_bytes(HD, BITS), SB = mx_scale_bytes(HD);
   constexpr int NL = TB / 1024;            // 1 KB loads of a tile of keys, and of values
   constexpr int KROW = HD * BITS / 8;      // bytes of a key
+  constexpr int AHEAD = ahead(HD), NSLOT = AHEAD + 1;
+  constexpr bool EARLY = AHEAD == 4;       // key fragments are read before the barrier
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
@@ -490,16 +511,26 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     return min(64, min(p.T, kv_len - f * p.T) - 64 * (tb + t - f * p.nt));
   };
 
-  f32x16 o[DB], s[2];
+  // byte offsets of this lane's fragments in a tile
+  int k_at[KS * BITS / 4], ks_at[2], v_at[4];
+#pragma unroll
+  for (int i = 0; i < KS * BITS / 4; ++i)   // 16-byte chunk 2 i + hh of row n32 (row 32 + n32: 32 KROW on)
+    k_at[i] = n32 * KROW + (((2 * i + hh) ^ swz<KROW>(n32)) << 4);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) ks_at[b] = row_key(b, n32) * (HD / 32);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v_at[k] = n32 * 128 + (((4 * hh + k) ^ swz<128>(n32)) << 4);
+
+  f32x16 o[DB], s[2], p_[2];   // p_: weights of the last VALU phase
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
-  bf16x8 pf[4];
+  float top = 0.f;             // largest score of the query's tile
 
   // value codes of position t to bf16: this thread HD / 8 keys of one dim
-  auto convert = [&](int t, int keys) __attribute__((always_inline)) {
+  auto convert = [&](int t, auto cut_c, int keys) __attribute__((always_inline)) {
     constexpr int E = HD / 8;
     const int dim = tid / (64 / E), k0 = E * (tid % (64 / E));
     const uint8_t* src = lds.v[t % NSLOT] + tid * (E * BITS / 8);
@@ -518,68 +549,105 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
 #pragma unroll
     for (int i = 0; i < E / 8; ++i) {
       u32x4 x = BITS == 8 ? mx_decode8<BITS>(w[2 * i], w[2 * i + 1], sc) : mx_decode8<BITS>(w[i], 0u, sc);
-      if (keys < 64) x = keep_first(x, keys - k0 - 8 * i);
+      if constexpr (decltype(cut_c)::value) x = keep_first(x, keys - k0 - 8 * i);
       *reinterpret_cast<u32x4*>(dst + 8 * ((k0 / 8 + i) ^ swz<128>(dim))) = x;
     }
   };
-
-  auto mfma_phase = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
-    constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
-    __builtin_amdgcn_s_setprio(1);
-    if constexpr (PV) {
-      const bf16_t* tv = lds.vb[(t - 1) & 1];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const int dim = 32 * db + n32;
-          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(tv + dim * 64 + 8 * ((4 * hh + k) ^ swz<128>(n32)));
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[db], 0, 0, 0);
-        }
-    }
-    if constexpr (QK) {
-      const uint8_t* tk = lds.k[t % NSLOT];
-      i32x8 kf[2][KS];
-      uint32_t sk[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int R = 32 * b + n32, key = row_key(b, n32);
-        if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(lds.ks[t % NSLOT] + 4 * key);
-        else sk[b] = *reinterpret_cast<const uint16_t*>(lds.ks[t % NSLOT] + 2 * key);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if constexpr (BITS == 8) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((4 * ks + hh) ^ swz<KROW>(R)) << 4));
-            const u32x4 y = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((4 * ks + 2 + hh) ^ swz<KROW>(R)) << 4));
-            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
-                              static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
-          } else {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + R * KROW + (((2 * ks + hh) ^ swz<KROW>(R)) << 4));
-            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]), 0, 0, 0, 0};
-          }
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < 2; ++b) score_block<HD, BITS>(kf[b], sk[b] >> (8 * hh), q, s[b]);
-    }
-    __builtin_amdgcn_s_setprio(0);
-    if constexpr (HD == 128) __builtin_amdgcn_sched_barrier(0);
+  const std::true_type yes;
+  const std::false_type no;
+  // (a tile that is not whole is written again with zeros past its keys)
+  auto trim = [&](int t) __attribute__((always_inline)) {
+    const int keys = keys_of(t);
+    if (keys < 64) convert(t, yes, keys);
   };
-
-  auto softmax = [&](int keys) __attribute__((always_inline)) {
-    if (keys < 64) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * hh + 16 * b + i >= keys) s[b][i] = -INFINITY;
-    }
+  auto tile_max = [&]() __attribute__((always_inline)) {
     float mx = -INFINITY;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-    mx = pair_max(mx) * c;
+    top = pair_max(mx);
+  };
+
+  // key fragments and scales of position t
+  i32x8 kf[2][KS];
+  uint32_t sk[2];
+  auto read_keys = [&](int t) __attribute__((always_inline)) {
+      const uint8_t* tk = &lds.k[0][0] + (t % NSLOT) * TB;
+      const uint8_t* tks = &lds.ks[0][0] + (t % NSLOT) * SB;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(tks + ks_at[b]);
+        else sk[b] = *reinterpret_cast<const uint16_t*>(tks + ks_at[b]);
+        sk[b] >>= 8 * hh;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (BITS == 8) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + k_at[2 * ks] + 32 * KROW * b);
+            const u32x4 y = *reinterpret_cast<const u32x4*>(tk + k_at[2 * ks + 1] + 32 * KROW * b);
+            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
+                              static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
+          } else {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + k_at[ks] + 32 * KROW * b);
+            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]), 0, 0, 0, 0};
+          }
+        }
+      }
+  };
+
+  auto mfma_phase = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
+    constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
+    __builtin_amdgcn_s_setprio(1);
+    bf16x8 vf[4][DB];
+    if constexpr (QK) {
+      if constexpr (!EARLY) read_keys(t);
+      scores<HD, BITS>(kf, sk, q, s);
+    }
+    if constexpr (PV) {
+      const uint8_t* tv = reinterpret_cast<const uint8_t*>(&lds.vb[0][0]) + ((t - 1) & 1) * (128 * HD);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) vf[k][db] = *reinterpret_cast<const bf16x8*>(tv + v_at[k] + 4096 * db);
+      const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+      bf16x8 pf[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 8 * (k & 1) + 2 * j;
+          w[j] = pack_bf16x2(p_[k >> 1][i], p_[k >> 1][i + 1]);
+          l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
+        }
+        pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][db], pf[k], o[db], 0, 0, 0);
+    }
+    if constexpr (QK) {
+      convert(t, no, 64);
+      tile_max();
+    }
+    asm volatile("" : "+v"(top), "+v"(l_run));
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // VALU phase: the weights of the scores
+  auto softmax = [&](int keys) __attribute__((always_inline)) {
+    if (keys < 64) {
+      const int left = keys - 32 * hh;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 16 * b + i < left ? s[b][i] : -INFINITY;
+      tile_max();
+    }
+    const float mx = top * c;
     // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
     // 2^8), so that o is seldom rescaled
     if (__any(mx > m_run + 8.0f)) {
@@ -592,30 +660,18 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
-    const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      uint32_t w[4];
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 8 * (k & 1) + 2 * j;
-        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run)),
-                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_run)));
-        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
-      }
-      pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-    }
-    if constexpr (HD == 128)
-      asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]), "+v"(l_run));
+      for (int i = 0; i < 16; ++i) p_[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m_run));
+    asm volatile("" : "+v"(p_[0]), "+v"(p_[1]));
   };
-  const std::true_type yes;
-  const std::false_type no;
 
   // ---- prologue: the positions ahead of the group's first VALU phase
 #pragma unroll 1
-  for (int u = 0; u < 3 + grp; ++u)
+  for (int u = 0; u < AHEAD + grp; ++u)
     if (u < n) stage(u);
-  if (3 + grp > n) wait_pairs(w0);
+  if (AHEAD + grp > n) wait_pairs(w0);
   else if (grp == 0) wait_pairs(w2);
   else wait_pairs(w3);
   __syncthreads();
@@ -623,37 +679,41 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     if (u < n) wait_pairs(w2);
     else wait_pairs(w0);
   };
-  const bool rows = qt * BQ + wave * 32 < S.q_len;   // else: the wave only stages and converts
-  if (grp == 0) {
-    if (rows) mfma_phase(0, no, yes);
+  if (qt * BQ + wave * 32 < S.q_len) {
+    if constexpr (EARLY) read_keys(0);
+    mfma_phase(0, no, yes);
+    trim(0);
 #pragma unroll 1
-    for (int t = 0; t < n; ++t) {
-      const int keys = keys_of(t);
-      if (t + 3 < n) stage(t + 3);
-      if (rows) softmax(keys);
-      convert(t, keys);
-      wait_next(t + 3);
-      __syncthreads();
-      if (rows) {
-        if (t + 1 < n) mfma_phase(t + 1, yes, yes);
-        else mfma_phase(n, yes, no);
+    for (int t = 0; t + 1 < n; ++t) {
+      if (grp == 1) {
+        wait_next(t + AHEAD);
+        __syncthreads();
       }
+      if (t + AHEAD + grp < n) stage(t + AHEAD + grp);
+      softmax(keys_of(t));
+      if constexpr (EARLY) read_keys(t + 1);
+      if (grp == 0) {
+        wait_next(t + AHEAD);
+        __syncthreads();
+      }
+      mfma_phase(t + 1, yes, yes);
+      trim(t + 1);
     }
-  } else {
-    convert(0, keys_of(0));
-    if (rows) mfma_phase(0, no, yes);
+    // the last position: nothing is left to request, and no scores follow
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (grp == 1) __syncthreads();
+    softmax(keys_of(n - 1));
+    if (grp == 0) __syncthreads();
+    mfma_phase(n, yes, no);
+  } else {   // no query of this wave exists: it only stages and converts
+    convert(0, yes, keys_of(0));
 #pragma unroll 1
     for (int t = 0; t < n; ++t) {
-      wait_next(t + 3);
+      if (grp == 0 && t + AHEAD < n) stage(t + AHEAD);
+      wait_next(t + AHEAD);
       __syncthreads();
-      if (t + 4 < n) stage(t + 4);
-      if (rows) softmax(keys_of(t));
-      if (t + 1 < n) {
-        convert(t + 1, keys_of(t + 1));
-        if (rows) mfma_phase(t + 1, yes, yes);
-      } else if (rows) {
-        mfma_phase(n, yes, no);
-      }
+      if (grp == 1 && t + AHEAD + 1 < n) stage(t + AHEAD + 1);
+      if (t + 1 < n) convert(t + 1, yes, keys_of(t + 1));
     }
   }
 
@@ -699,7 +759,7 @@ __device__ __forceinline__ int item_stream(const AttnArgs& a, int item) {
 
 // One workgroup per item, each XCD a contiguous range of them.
 template <int HD, int BITS>
-__global__ __launch_bounds__(NTHR, HD == 64 ? 4 : 1) void attn_mx_kernel(const MxLargeArgs x) {
+__global__ __launch_bounds__(NTHR, 1) void attn_mx_kernel(const MxLargeArgs x) {
   __shared__ __attribute__((aligned(1024))) LargeLds<HD, BITS> lds;
   const AttnArgs& a = x.a;
   const int xcd = blockIdx.x % kNumXcd;
