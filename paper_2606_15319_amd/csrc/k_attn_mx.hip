@@ -89,8 +89,7 @@ __device__ __forceinline__ void split_query(const uint4 (&raw)[2], i32x8& hi, i3
 
 // Query row at qp (its head's first dim); hh: lane / 32
 template <int HD>
-__device__ __forceinline__ void load_query(const bf16_t* qp, int hh, Query<HD>& q) {
-  uint4 raw[HD / 64][2][2];
+__device__ __forceinline__ void read_query(const bf16_t* qp, int hh, uint4 (&raw)[HD / 64][2][2]) {
 #pragma unroll
   for (int ks = 0; ks < HD / 64; ++ks)
 #pragma unroll
@@ -98,12 +97,29 @@ __device__ __forceinline__ void load_query(const bf16_t* qp, int hh, Query<HD>& 
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         raw[ks][b][i] = *reinterpret_cast<const uint4*>(qp + 64 * ks + 32 * b + 16 * hh + 8 * i);
+}
+template <int HD>
+__device__ __forceinline__ void split_row(const uint4 (&raw)[HD / 64][2][2], int hh, Query<HD>& q) {
 #pragma unroll
   for (int ks = 0; ks < HD / 64; ++ks) {
     int s0, s1;
     split_query(raw[ks][0], q.hi[ks], q.lo[ks], 0, s0);
     split_query(raw[ks][1], q.hi[ks], q.lo[ks], 4, s1);
     q.sc[ks] = hh ? s1 : s0;
+  }
+}
+
+// Key fragment of the 64-dim step ks from the rows at tk; at: byte offsets of this
+// lane's 16-byte chunks.
+template <int BITS>
+__device__ __forceinline__ i32x8 key_fragment(const uint8_t* tk, const int* at, int ks) {
+  if constexpr (BITS == 8) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(tk + at[2 * ks]), y = *reinterpret_cast<const u32x4*>(tk + at[2 * ks + 1]);
+    return i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
+                 static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
+  } else {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(tk + at[ks]);
+    return i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]), 0, 0, 0, 0};
   }
 }
 
@@ -134,70 +150,50 @@ __device__ __forceinline__ void scores(const i32x8 (&k)[2][HD / 64], const uint3
   }
 }
 
+// 16-byte chunk c of an LDS row of ROWB bytes sits at chunk c ^ swz(r): 16 rows then
+// cover every bank for a fixed c.
+template <int ROWB>
+__device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 16 - 1); }
+
 // ------------------------------------------------------------- few queries
 // A workgroup takes 32 rows of one (stream, head) and a cut of its key tiles, each of
-// its four waves every fourth tile; the waves meet in LDS.  Tiles are read straight
-// from memory (a wave's tile is its own), the next one's bytes while this one is
-// computed.  Cuts of one row tile leave partial results (unnormalised o, running
-// maximum, denominator) that a second kernel joins.
+// its four waves every fourth tile; the waves meet in LDS.  A wave's tiles are its own:
+// they come by direct loads into a ring of 32 KB a wave, 2 to 8 tiles, so that a CU
+// has 128 KB under way whatever the format, and nobody waits for another wave.  Cuts of
+// one row tile leave partial results (unnormalised o, running maximum, denominator)
+// that a second kernel joins.
 constexpr int SM_BQ = 32;
 constexpr int SM_WAVES = 4;
 
 template <int HD, int BITS>
-struct TileBytes {
-  i32x8 k[2][HD / 64];
-  uint32_t ks[2];
-  u32x4 v[HD / 32][BITS / 4];
-  uint32_t vs[HD / 32];
+struct Ring {
+  static constexpr int TILES = 32768 / (2 * mx_tile_bytes(HD, BITS));
+  struct Tile {
+    uint8_t k[mx_tile_bytes(HD, BITS)];     // row R = 32 b + r: key row_key(b, r), chunks swizzled
+    uint8_t v[mx_tile_bytes(HD, BITS)];     // row: dim, chunks swizzled
+    uint8_t ks[mx_scale_bytes(HD)], vs[mx_scale_bytes(HD)];
+  };
+  Tile t[SM_WAVES][TILES];
+};
+template <int HD>
+struct Meeting {
+  float o[SM_WAVES][SM_BQ][HD];
+  float m[SM_WAVES][SM_BQ], l[SM_WAVES][SM_BQ];
 };
 
 template <int HD, int BITS>
-__device__ __forceinline__ void load_tile(const MxPages& p, size_t tile, int n, int hh, TileBytes<HD, BITS>& t) {
-  const uint8_t* kc = p.k + tile * mx_tile_bytes(HD, BITS);
-  const uint8_t* vc = p.v + tile * mx_tile_bytes(HD, BITS);
-  const uint8_t* ks = p.ks + tile * mx_scale_bytes(HD);
-  const uint8_t* vs = p.vs + tile * mx_scale_bytes(HD);
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int key = row_key(b, n);
-    const uint8_t* row = kc + key * (HD * BITS / 8);
-#pragma unroll
-    for (int s = 0; s < HD / 64; ++s) {
-      if constexpr (BITS == 8) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(row + 64 * s + 16 * hh);
-        const u32x4 y = *reinterpret_cast<const u32x4*>(row + 64 * s + 32 + 16 * hh);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          t.k[b][s][i] = static_cast<int>(x[i]);
-          t.k[b][s][4 + i] = static_cast<int>(y[i]);
-        }
-      } else {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(row + 32 * s + 16 * hh);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          t.k[b][s][i] = static_cast<int>(x[i]);
-          t.k[b][s][4 + i] = 0;
-        }
-      }
-    }
-    if constexpr (HD == 128) t.ks[b] = *reinterpret_cast<const uint32_t*>(ks + 4 * key);
-    else t.ks[b] = *reinterpret_cast<const uint16_t*>(ks + 2 * key);
-  }
-#pragma unroll
-  for (int db = 0; db < HD / 32; ++db) {
-    const int dim = 32 * db + n;
-#pragma unroll
-    for (int i = 0; i < BITS / 4; ++i)
-      t.v[db][i] = *reinterpret_cast<const u32x4*>(vc + dim * (8 * BITS) + hh * (4 * BITS) + 16 * i);
-    t.vs[db] = vs[hh * HD + dim];
-  }
-}
-
-template <int HD, int BITS>
 __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const MxSmallArgs a) {
-  constexpr int DB = HD / 32;
-  __shared__ __attribute__((aligned(16))) float part[SM_WAVES][SM_BQ][HD];
-  __shared__ float part_m[SM_WAVES][SM_BQ], part_l[SM_WAVES][SM_BQ];
+  constexpr int DB = HD / 32, KS = HD / 64;
+  constexpr int TB = mx_tile_bytes(HD, BITS), SB = mx_scale_bytes(HD);
+  constexpr int NL = TB / 1024;                        // loads of a tile of keys, and of values
+  constexpr int KROW = HD * BITS / 8, VROW = 8 * BITS;   // bytes of a key, and of a dim's 64 keys
+  constexpr int NT = Ring<HD, BITS>::TILES;
+  constexpr int LOADS = 2 * NL + 2;
+  static_assert((NT - 1) * LOADS < 64, "the counter of loads under way has six bits");
+  __shared__ union __attribute__((aligned(1024))) Lds {
+    Ring<HD, BITS> ring;
+    Meeting<HD> part;
+  } lds;
   const MxPages& p = a.p;
   const int L = (static_cast<int>(blockIdx.x) % kNumXcd) * a.per_xcd + static_cast<int>(blockIdx.x) / kNumXcd;
   if (L >= a.total_items) return;
@@ -213,8 +209,67 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   const int n = lane & 31, hh = lane >> 5;
   const float c = a.scale_log2;
 
+  // pages of 64 frames, a lane each, from the frame of the next tile requested on
+  const int last_frame = static_cast<int>(fdiv(static_cast<uint32_t>(S.kv_len - 1), p.fT));
+  const int32_t* pt = p.page_table + static_cast<size_t>(S.row) * p.max_frames;
+  auto page_window = [&](int f0) __attribute__((always_inline)) {
+    return min(max(pt[min(f0 + lane, last_frame)], 0), p.n_pages - 1);
+  };
+  int pw0 = static_cast<int>(fdiv(static_cast<uint32_t>(min(tb + wave, te - 1)), p.fnt));
+  int pw = page_window(pw0);
+  const bf16_t* qp = a.q + static_cast<size_t>(S.q_off + min(qt * SM_BQ + n, S.q_len - 1)) * a.ld + h * HD;
+  uint4 raw[KS][2][2];
+  read_query<HD>(qp, hh, raw);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)   // the row and the pages have landed before the first direct load
+    asm volatile("" : "+v"(raw[ks][0][0].x), "+v"(raw[ks][0][1].x), "+v"(raw[ks][1][0].x), "+v"(raw[ks][1][1].x),
+                 "+v"(pw));
+
+  // direct loads.  Load j of the keys fills LDS rows j (1024 / KROW) ..; of the values alike.
+  uint32_t k_off[NL], v_off[NL];
+#pragma unroll
+  for (int j = 0; j < NL; ++j) {
+    const int R = j * (1024 / KROW) + lane / (KROW / 16), D = j * (1024 / VROW) + lane / (VROW / 16);
+    k_off[j] = static_cast<uint32_t>(row_key(R >> 5, R & 31) * KROW + (((lane % (KROW / 16)) ^ swz<KROW>(R)) << 4));
+    v_off[j] = static_cast<uint32_t>(D * VROW + (((lane % (VROW / 16)) ^ swz<VROW>(D)) << 4));
+  }
+  const uint32_t s_off = static_cast<uint32_t>(lane * 4);
+  typename Ring<HD, BITS>::Tile* ring = lds.ring.t[wave];
+  const uint32_t lds_ring = lds_address(ring);
+  auto fetch = [&](int t, int slot) __attribute__((always_inline)) {
+    const int f = static_cast<int>(fdiv(static_cast<uint32_t>(t), p.fnt));
+    if (f - pw0 >= 64) {
+      pw0 = f;
+      pw = page_window(f);
+      asm volatile("" : "+v"(pw));
+    }
+    const size_t tile = mx_tile(p, __builtin_amdgcn_readlane(pw, f - pw0), h, t - f * p.nt);
+    const uint32_t at = lds_ring + static_cast<uint32_t>(slot) * sizeof(typename Ring<HD, BITS>::Tile);
+    const char* kc = reinterpret_cast<const char*>(p.k) + tile * TB;
+    const char* vc = reinterpret_cast<const char*>(p.v) + tile * TB;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) lds_dma16(kc, k_off[j], at + 1024u * j);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) lds_dma16(vc, v_off[j], at + TB + 1024u * j);
+    if (lane < SB / 4) {
+      lds_dma4(reinterpret_cast<const char*>(p.ks) + tile * SB, s_off, at + 2 * TB);
+      lds_dma4(reinterpret_cast<const char*>(p.vs) + tile * SB, s_off, at + 2 * TB + SB);
+    }
+  };
+#pragma unroll 1
+  for (int i = 0; i < NT; ++i)
+    if (tb + wave + SM_WAVES * i < te) fetch(tb + wave + SM_WAVES * i, i);
+
   Query<HD> q;
-  load_query<HD>(a.q + static_cast<size_t>(S.q_off + min(qt * SM_BQ + n, S.q_len - 1)) * a.ld + h * HD, hh, q);
+  split_row<HD>(raw, hh, q);
+  // byte offsets of this lane's fragments in a tile
+  int k_at[KS * BITS / 4], ks_at[2], v_at[BITS / 4];
+#pragma unroll
+  for (int i = 0; i < KS * BITS / 4; ++i) k_at[i] = n * KROW + (((2 * i + hh) ^ swz<KROW>(n)) << 4);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) ks_at[b] = row_key(b, n) * (HD / 32);
+#pragma unroll
+  for (int i = 0; i < BITS / 4; ++i) v_at[i] = n * VROW + (((hh * (BITS / 4) + i) ^ swz<VROW>(n)) << 4);
 
   f32x16 o[DB];
 #pragma unroll
@@ -223,21 +278,38 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   // (it starts finite, so that scores that all overflowed to -inf weigh nothing)
   float m_run = kNoMax, l_run = 0.f;
-
-  // tile index and number of keys of tile t (a tile past the range: the last one's)
-  auto locate = [&](int t, int& keys) __attribute__((always_inline)) {
-    const int f = static_cast<int>(fdiv(static_cast<uint32_t>(t), p.fnt)), ti = t - f * p.nt;
-    keys = min(64, min(p.T, S.kv_len - f * p.T) - 64 * ti);
-    return mx_tile(p, mx_read_page(p, S.row, f), h, ti);
-  };
-  TileBytes<HD, BITS> now, next;
-  int keys = 0, keys_next = 0;
-  if (tb + wave < te) load_tile<HD, BITS>(p, locate(tb + wave, keys), n, hh, now);
+  int slot = 0;
+#pragma unroll 1
   for (int t = tb + wave; t < te; t += SM_WAVES) {
-    if (t + SM_WAVES < te) load_tile<HD, BITS>(p, locate(t + SM_WAVES, keys_next), n, hh, next);
+    // this tile has landed: those after it are under way, NT - 1 of them but at the end
+    if (t + SM_WAVES * (NT - 1) < te) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NT - 1) * LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const typename Ring<HD, BITS>::Tile& tile = ring[slot];
+    i32x8 kf[2][KS];
+    uint32_t sk[2], vsb[DB];
+    u32x4 vw[DB][BITS / 4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(tile.ks + ks_at[b]);
+      else sk[b] = *reinterpret_cast<const uint16_t*>(tile.ks + ks_at[b]);
+      sk[b] >>= 8 * hh;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[b][ks] = key_fragment<BITS>(tile.k + 32 * KROW * b, k_at, ks);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+      for (int i = 0; i < BITS / 4; ++i) vw[db][i] = *reinterpret_cast<const u32x4*>(tile.v + 32 * VROW * db + v_at[i]);
+      vsb[db] = tile.vs[hh * HD + 32 * db + n];
+    }
+    // everything read: the slot takes the tile after those under way
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (t + SM_WAVES * NT < te) fetch(t + SM_WAVES * NT, slot);
+    slot = slot + 1 == NT ? 0 : slot + 1;
+    const int f = static_cast<int>(fdiv(static_cast<uint32_t>(t), p.fnt));
+    const int keys = min(64, min(p.T, S.kv_len - f * p.T) - 64 * (t - f * p.nt));
     f32x16 s[2];
-    const uint32_t sk[2] = {now.ks[0] >> (8 * hh), now.ks[1] >> (8 * hh)};
-    scores<HD, BITS>(now.k, sk, q, s);
+    scores<HD, BITS>(kf, sk, q, s);
     if (keys < 64) {
       const int left = keys - 32 * hh;
 #pragma unroll
@@ -274,20 +346,19 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      const float sc = mx_scale(now.vs[db]);
+      const float sc = mx_scale(vsb[db]);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         u32x4 x;
-        if constexpr (BITS == 8) x = mx_decode8<8>(now.v[db][k >> 1][2 * (k & 1)], now.v[db][k >> 1][2 * (k & 1) + 1], sc);
-        else x = mx_decode8<4>(now.v[db][0][k], 0u, sc);
+        if constexpr (BITS == 8) x = mx_decode8<8>(vw[db][k >> 1][2 * (k & 1)], vw[db][k >> 1][2 * (k & 1) + 1], sc);
+        else x = mx_decode8<4>(vw[db][0][k], 0u, sc);
         // values past the end are zero: whatever the page holds there would meet a zero weight
         if (keys < 64) x = keep_first(x, keys - 32 * hh - 8 * k);
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf[k], o[db], 0, 0, 0);
       }
     }
-    now = next;
-    keys = keys_next;
   }
+  __syncthreads();   // the rings make room for the results
 
   // the waves' results meet: o = sum_w 2^(m_w - M) o_w (a wave without tiles adds nothing)
   const float l_tot = pair_sum(l_run);
@@ -296,12 +367,12 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
 #pragma unroll
     for (int g = 0; g < 4; ++g) {   // dims 32 db + 8 g + 4 hh .. + 4; 16-byte chunks XOR-swizzled by row
       const int ch = 8 * db + 2 * g + hh;
-      *reinterpret_cast<float4*>(&part[wave][n][4 * (ch ^ (n & 15))]) =
+      *reinterpret_cast<float4*>(&lds.part.o[wave][n][4 * (ch ^ (n & 15))]) =
           make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
     }
   if (hh == 0) {
-    part_m[wave][n] = m_run;
-    part_l[wave][n] = l_tot;
+    lds.part.m[wave][n] = m_run;
+    lds.part.l[wave][n] = l_tot;
   }
   __syncthreads();
   constexpr int TPR = HD / 4;
@@ -309,17 +380,17 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     const int row = i / TPR, c4 = i % TPR;
     const int ql = qt * SM_BQ + row;
     if (ql >= S.q_len) break;
-    float M = part_m[0][row];
+    float M = lds.part.m[0][row];
 #pragma unroll
-    for (int w = 1; w < SM_WAVES; ++w) M = fmaxf(M, part_m[w][row]);
+    for (int w = 1; w < SM_WAVES; ++w) M = fmaxf(M, lds.part.m[w][row]);
     float l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < SM_WAVES; ++w) {
       if (tb + w >= te) break;
-      const float wgt = __builtin_amdgcn_exp2f(part_m[w][row] - M);
-      const float4 x = *reinterpret_cast<const float4*>(&part[w][row][4 * (c4 ^ (row & 15))]);
-      l += wgt * part_l[w][row];
+      const float wgt = __builtin_amdgcn_exp2f(lds.part.m[w][row] - M);
+      const float4 x = *reinterpret_cast<const float4*>(&lds.part.o[w][row][4 * (c4 ^ (row & 15))]);
+      l += wgt * lds.part.l[w][row];
       acc.x += wgt * x.x;
       acc.y += wgt * x.y;
       acc.z += wgt * x.z;
@@ -360,9 +431,11 @@ __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) 
                    : P.part_begin + (static_cast<size_t>(h) * P.pieces + j - own) * P.q_len + r;
   };
   float M = kNoMax;
+#pragma unroll 8
   for (int j = 0; j < all; ++j) M = fmaxf(M, a.part_ml[slot(j)].x);
   float l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
   for (int j = 0; j < all; ++j) {
     const size_t at = slot(j);
     const float2 ml = a.part_ml[at];
@@ -394,11 +467,6 @@ static_assert(sizeof(MxLargeArgs) <= 4096, "arguments must fit the kernel-argume
 constexpr int BQ = 256;
 constexpr int NTHR = 512;
 
-
-// 16-byte chunk c of an LDS row of ROWB bytes sits at chunk c ^ swz(r): 16 rows then
-// cover every bank for a fixed c.
-template <int ROWB>
-__device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 16 - 1); }
 
 // Tiles requested ahead of the one computed.  At d = 64 key fragments are read before
 // the barrier that their products follow (they have to have landed one barrier sooner):
@@ -444,8 +512,12 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
   const int kv_len = S.base_off;
 
   Query<HD> q;
-  load_query<HD>(a.q + static_cast<size_t>(S.q_off + min(qt * BQ + wave * 32 + n32, S.q_len - 1)) * a.ldq + h * HD,
-                 hh, q);
+  {
+    uint4 raw[KS][2][2];
+    read_query<HD>(a.q + static_cast<size_t>(S.q_off + min(qt * BQ + wave * 32 + n32, S.q_len - 1)) * a.ldq + h * HD,
+                   hh, raw);
+    split_row<HD>(raw, hh, q);
+  }
 
   // ---- staging by direct loads.  Eight loads a tile: every wave one of keys and one of
   // values; four: waves 0-3 keys, 4-7 values; two: waves 0, 1 and 4, 5.
@@ -581,17 +653,7 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
         else sk[b] = *reinterpret_cast<const uint16_t*>(tks + ks_at[b]);
         sk[b] >>= 8 * hh;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if constexpr (BITS == 8) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + k_at[2 * ks] + 32 * KROW * b);
-            const u32x4 y = *reinterpret_cast<const u32x4*>(tk + k_at[2 * ks + 1] + 32 * KROW * b);
-            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
-                              static_cast<int>(y[0]), static_cast<int>(y[1]), static_cast<int>(y[2]), static_cast<int>(y[3])};
-          } else {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(tk + k_at[ks] + 32 * KROW * b);
-            kf[b][ks] = i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]), 0, 0, 0, 0};
-          }
-        }
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = key_fragment<BITS>(tk + 32 * KROW * b, k_at, ks);
       }
   };
 
@@ -856,31 +918,47 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a, bool join) {
 }
 
 constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
+constexpr int kSmallStart = 4;     // a workgroup's start and end, in tiles of a wave
 
-// Cuts the spans' key tiles so that the workgroups fill one round of the GPU and the
-// partial rows fit max_rows.  True when some span leaves partial results.
+// Cuts the spans' key tiles: the length of a cut with the earliest estimated end among
+// a few, such that the partial rows fit max_rows.  True when some span leaves partial
+// results.
 bool plan_small(MxSmallArgs& a, int64_t max_rows) {
   int64_t cost = 0;
-  int most = 0;
+  int most = 1;
   for (int i = 0; i < a.n_spans; ++i) {
     MxSpan& s = a.s[i];
     s.n_qtiles = (s.q_len + SM_BQ - 1) / SM_BQ;
     cost += static_cast<int64_t>(s.n_qtiles) * a.p.H * (s.tile1 - s.tile0);
     most = std::max(most, s.tile1 - s.tile0);
   }
-  auto fits = [&](int w) {
-    int64_t items = 0, rows = 0;
+  // In tiles of a wave: workgroups of one round end with the longest; of several, the
+  // CUs take them as they come.
+  auto end = [&](int w) {
+    int64_t items = 0, rows = 0, sum = 0;
+    int longest = 0;
     for (int i = 0; i < a.n_spans; ++i) {
       const MxSpan& s = a.s[i];
-      const int64_t pieces = std::max(1, (s.tile1 - s.tile0 + w - 1) / w);
-      items += s.n_qtiles * pieces * a.p.H;
-      if (pieces > 1 || a.shared) rows += s.q_len * pieces * a.p.H;
+      const int tiles = s.tile1 - s.tile0, pieces = std::max(1, (tiles + w - 1) / w);
+      const int one = kSmallStart + ((tiles + pieces - 1) / pieces + SM_WAVES - 1) / SM_WAVES;
+      const int64_t n = static_cast<int64_t>(s.n_qtiles) * a.p.H * pieces;
+      items += n;
+      sum += n * one;
+      longest = std::max(longest, one);
+      if (pieces > 1 || a.shared) rows += static_cast<int64_t>(s.q_len) * pieces * a.p.H;
     }
-    return items <= kSmallRound && rows <= max_rows;
+    if (rows > max_rows) return INT64_MAX;
+    return items <= kSmallRound ? static_cast<int64_t>(2 * longest) : 2 * sum / kSmallRound + longest;
   };
-  int W = static_cast<int>(std::max<int64_t>(SM_WAVES, (cost + kSmallRound - 1) / kSmallRound));
-  while (W < most && !fits(W)) W += std::max(1, W / 16);
-  W = std::min(W, std::max(most, 1));
+  int W = most;
+  int64_t best = end(most);
+  for (int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / kSmallRound)); w < most; w += std::max(SM_WAVES, w / 4)) {
+    const int64_t e = end(w);
+    if (e < best) {
+      best = e;
+      W = w;
+    }
+  }
   bool join = false;
   int64_t items = 0, rows = 0;
   for (int i = 0; i < a.n_spans; ++i) {

@@ -261,17 +261,24 @@ struct ReadArgs {
   bf16_t* v;
   const int32_t* page_table;
   int max_frames, n_pages;
-  FastDiv fH;
+  int tiles, total;         // tiles of the streams, and of all heads
+  FastDiv ftiles;
   RowStreams rs;            // row_begin: first tile of the stream, len and cache_len in tokens
 };
 static_assert(sizeof(ReadArgs) <= 4096, "arguments must fit the kernel-argument buffer");
 
-// One tile of 64 keys of one head: 16 codes a thread and step.
+// One tile of 64 keys of one head, 8 codes a thread and step, so that every store
+// instruction of a wave writes whole runs of lines.
 template <int HD, int BITS>
 __global__ __launch_bounds__(256) void kv_read_mx_kernel(const ReadArgs a) {
   const MxPages& p = a.p;
-  const int g = static_cast<int>(fdiv(blockIdx.x, a.fH));
-  const int h = static_cast<int>(blockIdx.x) - g * p.H;
+  // each XCD takes a run of one head's tiles after the other: the values of neighbouring
+  // tiles share lines of dst's transposed rows, which meet in one L2
+  const int per = (a.total + kNumXcd - 1) / kNumXcd;
+  const int L = static_cast<int>(blockIdx.x % kNumXcd) * per + static_cast<int>(blockIdx.x / kNumXcd);
+  if (static_cast<int>(blockIdx.x / kNumXcd) >= per || L >= a.total) return;
+  const int h = static_cast<int>(fdiv(static_cast<uint32_t>(L), a.ftiles));
+  const int g = L - h * a.tiles;
   const int b = stream_of(a.rs, g);
   const RowStream s = a.rs.s[b];
   const int t = g - s.row_begin;                  // tile of the stream's range
@@ -283,53 +290,42 @@ __global__ __launch_bounds__(256) void kv_read_mx_kernel(const ReadArgs a) {
   const int dst = write_page(a.page_table[static_cast<size_t>(b) * a.max_frames + fr], a.n_pages);
   if (dst < 0) return;
   const size_t tile = mx_tile(p, src, h, ti);
-  constexpr int STEPS = HD / 64;                  // 64 HD values: 16 a thread and step
-  constexpr int CB = 2 * BITS;                    // bytes of 16 codes
+  constexpr int STEPS = HD / 32;                  // 64 HD values: 8 a thread and step
   const uint8_t* kc = p.k + tile * mx_tile_bytes(HD, BITS);
   const uint8_t* vc = p.v + tile * mx_tile_bytes(HD, BITS);
-  uint4 kw[STEPS], vw[STEPS];
+  uint2 kw[STEPS], vw[STEPS];
   uint32_t ksb[STEPS], vsb[STEPS];
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int c = threadIdx.x + 256 * i;
     if constexpr (BITS == 8) {
-      kw[i] = *reinterpret_cast<const uint4*>(kc + c * CB);
-      vw[i] = *reinterpret_cast<const uint4*>(vc + c * CB);
+      kw[i] = *reinterpret_cast<const uint2*>(kc + c * 8);
+      vw[i] = *reinterpret_cast<const uint2*>(vc + c * 8);
     } else {
-      const uint2 x = *reinterpret_cast<const uint2*>(kc + c * CB), y = *reinterpret_cast<const uint2*>(vc + c * CB);
-      kw[i] = make_uint4(x.x, x.y, 0u, 0u);
-      vw[i] = make_uint4(y.x, y.y, 0u, 0u);
+      kw[i] = make_uint2(*reinterpret_cast<const uint32_t*>(kc + c * 4), 0u);
+      vw[i] = make_uint2(*reinterpret_cast<const uint32_t*>(vc + c * 4), 0u);
     }
-    ksb[i] = p.ks[tile * mx_scale_bytes(HD) + c / 2];                                  // 32 dims of a key: 2 threads
-    vsb[i] = p.vs[tile * mx_scale_bytes(HD) + ((c & 3) >> 1) * HD + (c >> 2)];        // 32 keys of a dim
+    ksb[i] = p.ks[tile * mx_scale_bytes(HD) + c / 4];                                 // 32 dims of a key: 4 threads
+    vsb[i] = p.vs[tile * mx_scale_bytes(HD) + ((c & 7) >> 2) * HD + (c >> 3)];       // 32 keys of a dim
   }
   const size_t head = (static_cast<size_t>(dst) * p.H + h) * p.T * HD;
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int c = threadIdx.x + 256 * i;
-    const int key = c / (HD / 16), e0 = 16 * (c % (HD / 16));
-    if (key < n) {
-      const float sc = mx_scale(ksb[i]);
-      uint4* d = reinterpret_cast<uint4*>(a.k + head + static_cast<size_t>(64 * ti + key) * HD + e0);
-      store_stream16(d, __builtin_bit_cast(uint4, mx_decode8<BITS>(kw[i].x, kw[i].y, sc)));
-      store_stream16(d + 1, __builtin_bit_cast(uint4, BITS == 8 ? mx_decode8<BITS>(kw[i].z, kw[i].w, sc)
-                                                                : mx_decode8<BITS>(kw[i].y, 0u, sc)));
-    }
-    const int dim = c >> 2, j0 = 16 * (c & 3);
-    const float sc = mx_scale(vsb[i]);
+    const int key = c / (HD / 8), e0 = 8 * (c % (HD / 8));
+    if (key < n)
+      store_stream16(a.k + head + static_cast<size_t>(64 * ti + key) * HD + e0,
+                     __builtin_bit_cast(uint4, mx_decode8<BITS>(kw[i].x, kw[i].y, mx_scale(ksb[i]))));
+    const int dim = c >> 3, j0 = 8 * (c & 7);
+    const u32x4 x = mx_decode8<BITS>(vw[i].x, vw[i].y, mx_scale(vsb[i]));
     bf16_t* d = a.v + head + static_cast<size_t>(dim) * p.T + 64 * ti + j0;
-    const u32x4 x[2] = {mx_decode8<BITS>(vw[i].x, vw[i].y, sc),
-                        BITS == 8 ? mx_decode8<BITS>(vw[i].z, vw[i].w, sc) : mx_decode8<BITS>(vw[i].y, 0u, sc)};
+    const int left = n - j0;
+    if (left >= 8) {
+      *reinterpret_cast<uint4*>(d) = __builtin_bit_cast(uint4, x);
+    } else {   // the tokens behind the last stay as they were
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int left = n - j0 - 8 * k;
-      if (left >= 8) {
-        store_stream16(d + 8 * k, __builtin_bit_cast(uint4, x[k]));
-      } else {   // the tokens behind the last stay as they were
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < left) d[8 * k + e] = static_cast<bf16_t>(x[k][e >> 1] >> (16 * (e & 1)));
-      }
+      for (int e = 0; e < 8; ++e)
+        if (e < left) d[e] = static_cast<bf16_t>(x[e >> 1] >> (16 * (e & 1)));
     }
   }
 }
@@ -394,7 +390,6 @@ hipError_t launch_kv_read_mx(hipStream_t st, const MxPages& p, bf16_t* k_pages, 
   a.page_table = page_table;
   a.max_frames = max_frames;
   a.n_pages = n_pages;
-  a.fH = make_fastdiv(p.H);
   a.rs = rs;
   int64_t tiles = 0;
   for (int i = 0; i < rs.n; ++i) {
@@ -402,7 +397,10 @@ hipError_t launch_kv_read_mx(hipStream_t st, const MxPages& p, bf16_t* k_pages, 
     tiles += mx_tiles(rs.s[i].len, p.T, p.nt);
   }
   if (tiles == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(tiles * p.H));
+  a.tiles = static_cast<int>(tiles);
+  a.total = static_cast<int>(tiles * p.H);
+  a.ftiles = make_fastdiv(static_cast<uint32_t>(tiles));
+  const dim3 grid(static_cast<unsigned>((a.total + kNumXcd - 1) / kNumXcd * kNumXcd));
   if (p.hd == 128) {
     if (p.bits == 8) hipLaunchKernelGGL((kv_read_mx_kernel<128, 8>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((kv_read_mx_kernel<128, 4>), grid, dim3(256), 0, st, a);
