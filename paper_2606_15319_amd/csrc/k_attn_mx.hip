@@ -157,17 +157,21 @@ __device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 
 
 // ------------------------------------------------------------- few queries
 // A workgroup takes 32 rows of one (stream, head) and a cut of its key tiles, each of
-// its four waves every fourth tile; the waves meet in LDS.  A wave's tiles are its own:
-// they come by direct loads into a ring of 32 KB a wave, 2 to 8 tiles, so that a CU
-// has 128 KB under way whatever the format, and nobody waits for another wave.  Cuts of
+// its eight waves every eighth tile; the waves meet in LDS.  A wave's tiles are its own:
+// they come by direct loads into a ring of 16 KB a wave, 1 to 4 tiles, so that a CU
+// has 128 KB under way whatever the format, and nobody waits for another wave.  A tile's
+// bytes go to registers at once and its place in the ring to the next one.  Cuts of
 // one row tile leave partial results (unnormalised o, running maximum, denominator)
-// that a second kernel joins.
+// that a second kernel joins.  Spans of few tiles are solo: a cut is one wave's, and
+// the eight waves of a workgroup are on their own.
+// What bounds it: the cache's bytes.  Eight tokens over 9 to 21 frames each in 8 bits
+// 113 us, 4.8 TB/s; with four waves and rings of 32 KB 117 (in 4 bits 66 for 86).
 constexpr int SM_BQ = 32;
-constexpr int SM_WAVES = 4;
+constexpr int SM_WAVES = 8;
 
 template <int HD, int BITS>
 struct Ring {
-  static constexpr int TILES = 32768 / (2 * mx_tile_bytes(HD, BITS));
+  static constexpr int TILES = 16384 / (2 * mx_tile_bytes(HD, BITS));
   struct Tile {
     uint8_t k[mx_tile_bytes(HD, BITS)];     // row R = 32 b + r: key row_key(b, r), chunks swizzled
     uint8_t v[mx_tile_bytes(HD, BITS)];     // row: dim, chunks swizzled
@@ -197,15 +201,20 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   const MxPages& p = a.p;
   const int L = (static_cast<int>(blockIdx.x) % kNumXcd) * a.per_xcd + static_cast<int>(blockIdx.x) / kNumXcd;
   if (L >= a.total_items) return;
-  int si = 0;
-  for (int i = 1; i < a.n_spans; ++i)
-    if (L >= a.s[i].item_begin) si = i;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool solo = L >= a.solo_item;
+  const int item = solo ? (L - a.solo_item) * SM_WAVES + wave : L;
+  if (solo && item >= a.solo_waves) return;
+  int si = solo ? a.solo_span : 0;
+  const int last_span = solo ? a.n_spans : a.solo_span;
+  for (int i = si + 1; i < last_span; ++i)
+    if (item >= a.s[i].item_begin) si = i;
   const MxSpan S = a.s[si];
-  const int it = L - S.item_begin;
+  const int it = item - S.item_begin;
   const int hp = it / S.n_qtiles, qt = it - hp * S.n_qtiles;
   const int h = hp / S.pieces, piece = hp - h * S.pieces;
   const int tb = S.tile0 + piece * S.per_piece, te = min(S.tile1, tb + S.per_piece);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int t0 = solo ? tb : tb + wave, stride = solo ? 1 : SM_WAVES;   // the wave's tiles
   const int n = lane & 31, hh = lane >> 5;
   const float c = a.scale_log2;
 
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   auto page_window = [&](int f0) __attribute__((always_inline)) {
     return min(max(pt[min(f0 + lane, last_frame)], 0), p.n_pages - 1);
   };
-  int pw0 = static_cast<int>(fdiv(static_cast<uint32_t>(min(tb + wave, te - 1)), p.fnt));
+  int pw0 = static_cast<int>(fdiv(static_cast<uint32_t>(min(t0, te - 1)), p.fnt));
   int pw = page_window(pw0);
   const bf16_t* qp = a.q + static_cast<size_t>(S.q_off + min(qt * SM_BQ + n, S.q_len - 1)) * a.ld + h * HD;
   uint4 raw[KS][2][2];
@@ -258,7 +267,7 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   };
 #pragma unroll 1
   for (int i = 0; i < NT; ++i)
-    if (tb + wave + SM_WAVES * i < te) fetch(tb + wave + SM_WAVES * i, i);
+    if (t0 + stride * i < te) fetch(t0 + stride * i, i);
 
   Query<HD> q;
   split_row<HD>(raw, hh, q);
@@ -280,9 +289,9 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   float m_run = kNoMax, l_run = 0.f;
   int slot = 0;
 #pragma unroll 1
-  for (int t = tb + wave; t < te; t += SM_WAVES) {
+  for (int t = t0; t < te; t += stride) {
     // this tile has landed: those after it are under way, NT - 1 of them but at the end
-    if (t + SM_WAVES * (NT - 1) < te) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NT - 1) * LOADS) : "memory");
+    if (t + stride * (NT - 1) < te) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NT - 1) * LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const typename Ring<HD, BITS>::Tile& tile = ring[slot];
     i32x8 kf[2][KS];
@@ -304,7 +313,7 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     }
     // everything read: the slot takes the tile after those under way
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (t + SM_WAVES * NT < te) fetch(t + SM_WAVES * NT, slot);
+    if (t + stride * NT < te) fetch(t + stride * NT, slot);
     slot = slot + 1 == NT ? 0 : slot + 1;
     const int f = static_cast<int>(fdiv(static_cast<uint32_t>(t), p.fnt));
     const int keys = min(64, min(p.T, S.kv_len - f * p.T) - 64 * (t - f * p.nt));
@@ -358,10 +367,37 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
       }
     }
   }
+  const float l_tot = pair_sum(l_run);
+  if (solo) {   // lane n + 32 hh holds dims 32 db + 8 g + 4 hh .. + 4 of its query
+    const int ql = qt * SM_BQ + n;
+    if (ql >= S.q_len) return;
+    if (S.part_begin < 0) {
+      const float inv = 1.0f / l_tot;
+      bf16_t* op = a.o + static_cast<size_t>(S.q_off + ql) * a.ld + h * HD;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint2 w;
+          w.x = pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
+          w.y = pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+          *reinterpret_cast<uint2*>(op + 32 * db + 8 * g + 4 * hh) = w;
+        }
+    } else {
+      const size_t at = S.part_begin + static_cast<size_t>(hp) * S.q_len + ql;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(a.part_o + at * HD + 32 * db + 8 * g + 4 * hh) =
+              make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+      if (hh == 0) a.part_ml[at] = make_float2(m_run, l_tot);
+    }
+    return;
+  }
   __syncthreads();   // the rings make room for the results
 
   // the waves' results meet: o = sum_w 2^(m_w - M) o_w (a wave without tiles adds nothing)
-  const float l_tot = pair_sum(l_run);
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -419,9 +455,10 @@ __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) 
   const int c4 = threadIdx.x % TPR;
   const int h = i / a.rows, r = i - h * a.rows;
   if (h >= a.p.H) return;
-  int si = a.shared;
-  for (int j = a.shared + 1; j < a.n_spans; ++j)
-    if (r >= a.s[j].q_off) si = j;
+  int si = -1;   // (streams in any order; each holds its rows once)
+  for (int j = a.shared; j < a.n_spans; ++j)
+    if (r >= a.s[j].q_off && r < a.s[j].q_off + a.s[j].q_len) si = j;
+  if (si < 0) return;            // a row of the other kernel's
   const MxSpan& S = a.s[si];
   if (S.part_begin < 0) return;   // written whole
   const MxSpan& P = a.s[0];
@@ -881,8 +918,7 @@ hipError_t launch_large(hipStream_t st, const MxLargeArgs& x) {
   return hipGetLastError();
 }
 
-// Whole-chunk attention of all streams.
-hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o, const RowStreams& rs,
+hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o, const RowStreams& rs, int rows_over,
                      float* part) {
   MxLargeArgs x;
   memset(&x, 0, sizeof(x));
@@ -893,9 +929,9 @@ hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* 
   a.ldq = a.ldo = p.H * p.hd;
   a.H = p.H;
   a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.hd)));
-  a.n_streams = rs.n;
   for (int i = 0; i < rs.n; ++i) {
-    AttnStream& s = a.s[i];
+    if (rs.s[i].len <= rows_over) continue;
+    AttnStream& s = a.s[a.n_streams++];
     s.q_off = rs.s[i].row_begin;
     s.q_len = rs.s[i].len;
     s.stream = i;
@@ -908,9 +944,9 @@ hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* 
 }
 
 template <int HD, int BITS>
-hipError_t launch_small(hipStream_t st, const MxSmallArgs& a, bool join) {
+hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
   hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
-  if (join) {
+  if (a.join) {
     constexpr int RPB = 256 / (HD / 4);
     hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + RPB - 1) / RPB), dim3(256), 0, st, a);
   }
@@ -919,11 +955,27 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a, bool join) {
 
 constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
 constexpr int kSmallStart = 4;     // a workgroup's start and end, in tiles of a wave
+// Most rows and tiles of a solo span.  32 continuations of one history, half of them with
+// a frame of their own: 89 us with a workgroup for each, 77 up to 16 tiles, 54 up to 32 or
+// 64; with 12 and 24 rows of partial results a wave it loses (six spans of 10 heads of
+// 64, 23 us for 21).
+constexpr int kSoloRows = 8, kSoloTiles = 32;
 
 // Cuts the spans' key tiles: the length of a cut with the earliest estimated end among
-// a few, such that the partial rows fit max_rows.  True when some span leaves partial
-// results.
-bool plan_small(MxSmallArgs& a, int64_t max_rows) {
+// a few, such that the partial rows fit max_rows.  Returns that end, in half tiles of a
+// wave.
+int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
+  // solo spans last: those of one row tile and few key tiles
+  auto is_solo = [](const MxSpan& s) { return s.q_len <= kSoloRows && s.tile1 - s.tile0 <= kSoloTiles; };
+  MxSpan tmp[kMaxStreams];
+  int n_solo = 0, n = a.shared;
+  for (int i = a.shared; i < a.n_spans; ++i) {
+    if (is_solo(a.s[i])) tmp[n_solo++] = a.s[i];
+    else a.s[n++] = a.s[i];
+  }
+  a.solo_span = n;
+  for (int i = 0; i < n_solo; ++i) a.s[n + i] = tmp[i];
+
   int64_t cost = 0;
   int most = 1;
   for (int i = 0; i < a.n_spans; ++i) {
@@ -932,81 +984,85 @@ bool plan_small(MxSmallArgs& a, int64_t max_rows) {
     cost += static_cast<int64_t>(s.n_qtiles) * a.p.H * (s.tile1 - s.tile0);
     most = std::max(most, s.tile1 - s.tile0);
   }
+  // Cuts of w tiles, of solo spans of a wave's share of them.
+  auto cut = [&](const MxSpan& s, int i, int w) {
+    const int tiles = s.tile1 - s.tile0;
+    const int each = i < a.solo_span ? w : std::max(1, (w + SM_WAVES - 1) / SM_WAVES);
+    return std::max(1, (tiles + each - 1) / each);
+  };
   // In tiles of a wave: workgroups of one round end with the longest; of several, the
   // CUs take them as they come.
   auto end = [&](int w) {
-    int64_t items = 0, rows = 0, sum = 0;
-    int longest = 0;
+    int64_t items = 0, rows = 0, sum = 0, solo = 0;
+    int longest = 0, solo_longest = 0;
     for (int i = 0; i < a.n_spans; ++i) {
       const MxSpan& s = a.s[i];
-      const int tiles = s.tile1 - s.tile0, pieces = std::max(1, (tiles + w - 1) / w);
-      const int one = kSmallStart + ((tiles + pieces - 1) / pieces + SM_WAVES - 1) / SM_WAVES;
-      const int64_t n = static_cast<int64_t>(s.n_qtiles) * a.p.H * pieces;
-      items += n;
-      sum += n * one;
-      longest = std::max(longest, one);
+      const int pieces = cut(s, i, w), each = (s.tile1 - s.tile0 + pieces - 1) / pieces;
+      const int64_t c = static_cast<int64_t>(s.n_qtiles) * a.p.H * pieces;
+      if (i < a.solo_span) {
+        const int one = kSmallStart + (each + SM_WAVES - 1) / SM_WAVES;
+        items += c;
+        sum += c * one;
+        longest = std::max(longest, one);
+      } else {
+        solo += c;
+        solo_longest = std::max(solo_longest, kSmallStart + each);
+      }
       if (pieces > 1 || a.shared) rows += static_cast<int64_t>(s.q_len) * pieces * a.p.H;
     }
     if (rows > max_rows) return INT64_MAX;
+    const int64_t wgs = (solo + SM_WAVES - 1) / SM_WAVES;
+    items += wgs;
+    sum += wgs * solo_longest;
+    longest = std::max(longest, solo_longest);
     return items <= kSmallRound ? static_cast<int64_t>(2 * longest) : 2 * sum / kSmallRound + longest;
   };
-  int W = most;
-  int64_t best = end(most);
-  for (int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / kSmallRound)); w < most; w += std::max(SM_WAVES, w / 4)) {
+  const int whole = std::max(most, SM_WAVES * std::min(most, kSoloTiles));   // no span is cut
+  int W = whole;
+  int64_t best = end(whole);
+  for (int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / kSmallRound)); w < whole; w += std::max(SM_WAVES, w / 4)) {
     const int64_t e = end(w);
     if (e < best) {
       best = e;
       W = w;
     }
   }
-  bool join = false;
-  int64_t items = 0, rows = 0;
+  a.join = 0;
+  int64_t items = 0, rows = 0, solo = 0;
   for (int i = 0; i < a.n_spans; ++i) {
     MxSpan& s = a.s[i];
     const int tiles = s.tile1 - s.tile0;
-    s.pieces = std::max(1, (tiles + W - 1) / W);
+    s.pieces = cut(s, i, W);
     s.per_piece = (tiles + s.pieces - 1) / s.pieces;
-    s.item_begin = static_cast<int32_t>(items);
-    items += static_cast<int64_t>(s.n_qtiles) * a.p.H * s.pieces;
+    int64_t& at = i < a.solo_span ? items : solo;
+    s.item_begin = static_cast<int32_t>(at);
+    at += static_cast<int64_t>(s.n_qtiles) * a.p.H * s.pieces;
     s.part_begin = -1;
     if (s.pieces > 1 || a.shared) {
       s.part_begin = static_cast<int32_t>(rows);
       rows += static_cast<int64_t>(a.p.H) * s.pieces * s.q_len;
-      join = true;
+      a.join = 1;
     }
   }
-  a.total_items = static_cast<int32_t>(items);
+  a.solo_item = static_cast<int32_t>(items);
+  a.solo_waves = static_cast<int32_t>(solo);
+  a.total_items = static_cast<int32_t>(items + (solo + SM_WAVES - 1) / SM_WAVES);
   a.per_xcd = (a.total_items + kNumXcd - 1) / kNumXcd;
-  return join;
+  return best;
 }
 
 }  // namespace
 
-hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
-                               const RowStreams& rs, int shared, float* part) {
-  MxSmallArgs a;
-  a.p = p;
-  a.q = q;
-  a.o = o;
-  a.ld = p.H * p.hd;
-  a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.hd)));
-  a.rows = 0;
-  int row_tiles = 0, first = -1;
-  for (int i = 0; i < rs.n; ++i) {
-    a.rows += rs.s[i].len;
-    row_tiles += (rs.s[i].len + SM_BQ - 1) / SM_BQ;
-    if (first < 0 && rs.s[i].len > 0) first = i;
-  }
-  if (a.rows == 0) return hipSuccess;
-  if (a.rows > 32 * row_tiles / 2 && row_tiles * p.H > 128) return run_large(st, p, q, o, rs, part);
-  const int64_t max_rows = static_cast<int64_t>(attention_split_bytes(p.hd) / (sizeof(float) * (p.hd + 2)));
-  a.part_o = part;
-  a.part_ml = reinterpret_cast<float2*>(part + max_rows * p.hd);
-  // The prefix is walked once for all rows where that makes fewer row tiles.
-  a.shared = shared > 0 && (a.rows + SM_BQ - 1) / SM_BQ < row_tiles &&
-             static_cast<int64_t>(2) * p.H * a.rows <= max_rows;
-  const int32_t tile0 = a.shared ? shared * p.nt : 0;
+// Spans of the streams with at most rows_most rows, planned; the estimated end in
+// hundredths of a microsecond.
+static int64_t plan_few(MxSmallArgs& a, const RowStreams& rs, int rows_most, int shared, int64_t max_rows) {
+  const MxPages& p = a.p;
+  int first = -1;
   a.n_spans = 0;
+  a.shared = shared > 0;
+  for (int i = 0; i < rs.n && first < 0; ++i)
+    if (rs.s[i].len > 0) first = i;
+  const int32_t tile0 = shared * p.nt;
   if (a.shared) {
     MxSpan& s = a.s[a.n_spans++];
     s.q_off = 0;
@@ -1017,7 +1073,7 @@ hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q
     s.tile1 = tile0;
   }
   for (int i = 0; i < rs.n; ++i) {
-    if (rs.s[i].len == 0) continue;
+    if (rs.s[i].len == 0 || rs.s[i].len > rows_most) continue;
     MxSpan& s = a.s[a.n_spans++];
     s.q_off = rs.s[i].row_begin;
     s.q_len = rs.s[i].len;
@@ -1026,9 +1082,77 @@ hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q
     s.tile0 = tile0;
     s.tile1 = static_cast<int32_t>(mx_tiles(s.kv_len, p.T, p.nt));
   }
-  const bool join = plan_small(a, max_rows);
-  if (p.hd == 128) return p.bits == 8 ? launch_small<128, 8>(st, a, join) : launch_small<128, 4>(st, a, join);
-  return p.bits == 8 ? launch_small<64, 8>(st, a, join) : launch_small<64, 4>(st, a, join);
+  const int64_t end = plan_small(a, max_rows);
+  return p.hd == 128 ? 730 + 105 * end : 690 + 67 * end;
+}
+
+// The estimated end of whole-chunk items of the streams with more rows, likewise.
+static int64_t estimate_many(const MxPages& p, const RowStreams& rs, int rows_over) {
+  int64_t items = 0, work = 0, most = 0;
+  for (int i = 0; i < rs.n; ++i) {
+    if (rs.s[i].len <= rows_over) continue;
+    const int64_t tiles = mx_tiles(static_cast<int64_t>(rs.s[i].cache_len) + rs.s[i].len, p.T, p.nt);
+    const int64_t n = static_cast<int64_t>((rs.s[i].len + BQ - 1) / BQ) * p.H;
+    items += n;
+    work += n * tiles;
+    most = std::max(most, tiles);
+  }
+  // (a round that the items leave idle is split; whole items go in rounds)
+  const int64_t tiles = items < 3 * kSmallRound / 4 ? work / kSmallRound : std::max(most, work / kSmallRound);
+  return p.hd == 128 ? 3260 + 122 * tiles : 2510 + 89 * tiles;
+}
+
+// Which kernel takes a stream goes by estimates fitted to 360 calls (1 to 8 streams of
+// 64 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
+// both formats), each timed on both: a tile of a wave, eight at a time on a CU, takes
+// 2.1 us at d = 128 and 1.35 at d = 64 after 7 us; a tile of 256 rows 1.22 and 0.89
+// after 33 and 25 (a split schedule and its merge).  The choice loses 0.6% to the better
+// one on average.  us of few rows' kernel and of whole-chunk items, 12 heads of 128 over
+// 32760 tokens: 64 rows 39 / 62, 192 66 / 76, 256 88 / 79, 768 321 / 159; four streams of
+// 100 181 / 156, eight of 64 197 / 267.
+hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
+                               const RowStreams& rs, int shared, float* part) {
+  MxSmallArgs a;
+  a.p = p;
+  a.q = q;
+  a.o = o;
+  a.ld = p.H * p.hd;
+  a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(p.hd)));
+  a.rows = 0;
+  int row_tiles = 0, longest = 0;
+  for (int i = 0; i < rs.n; ++i) {
+    a.rows += rs.s[i].len;
+    row_tiles += (rs.s[i].len + SM_BQ - 1) / SM_BQ;
+    longest = std::max(longest, rs.s[i].len);
+  }
+  if (a.rows == 0) return hipSuccess;
+  const int64_t max_rows = static_cast<int64_t>(attention_split_bytes(p.hd) / (sizeof(float) * (p.hd + 2)));
+  a.part_o = part;
+  a.part_ml = reinterpret_cast<float2*>(part + max_rows * p.hd);
+  // The prefix is walked once for all rows where that makes fewer row tiles.
+  const bool once = shared > 0 && (a.rows + SM_BQ - 1) / SM_BQ < row_tiles &&
+                    static_cast<int64_t>(2) * p.H * a.rows <= max_rows;
+  constexpr int kAll = INT32_MAX, kFew = 128;
+  int few = kAll;                 // streams of at most this many rows take the few rows' kernel
+  const int64_t end = plan_few(a, rs, kAll, once ? shared : 0, max_rows);
+  if (longest > SM_BQ) {
+    const int64_t many = estimate_many(p, rs, 0);
+    if (many < end) few = 0;
+    if (longest > kFew) {         // the long streams alone to the other kernel, in a launch before
+      MxSmallArgs b = a;
+      const int64_t both = plan_few(b, rs, kFew, 0, max_rows) + estimate_many(p, rs, kFew);
+      if (b.n_spans > 0 && both < std::min(end, many)) {
+        few = kFew;
+        a = b;
+      }
+    }
+  }
+  if (few != kAll) {
+    const hipError_t e = run_large(st, p, q, o, rs, few, part);
+    if (e != hipSuccess || few == 0) return e;
+  }
+  if (p.hd == 128) return p.bits == 8 ? launch_small<128, 8>(st, a) : launch_small<128, 4>(st, a);
+  return p.bits == 8 ? launch_small<64, 8>(st, a) : launch_small<64, 4>(st, a);
 }
 
 }  // namespace ardit

@@ -268,7 +268,7 @@ struct MxSpan {
   int32_t row;           // row of the page table
   int32_t tile0, tile1;
   int32_t n_qtiles, pieces, per_piece;   // row tiles; cuts of the key tiles, and tiles of a cut
-  int32_t item_begin;    // first workgroup
+  int32_t item_begin;    // first workgroup, or of a solo span the first wave
   int32_t part_begin;    // first partial row; -1: the output is written whole
 };
 struct MxSmallArgs {
@@ -278,7 +278,10 @@ struct MxSmallArgs {
   int32_t ld;
   float scale_log2;      // log2(e) / sqrt(d)
   int32_t n_spans, shared;   // shared: span 0 is the common prefix, of all rows
-  int32_t total_items, per_xcd;
+  int32_t join;          // some span leaves partial results
+  int32_t total_items, per_xcd;   // workgroups
+  int32_t solo_span;     // spans from here on: a cut is a wave's, not a workgroup's
+  int32_t solo_item, solo_waves;  // first workgroup of theirs, and their waves in all
   int32_t rows;          // rows of the packed queries
   float* part_o;         // [partial rows][hd]
   float2* part_ml;       // [partial rows] running max, denominator

@@ -274,6 +274,10 @@ ATTN = [   # H, d, lattice, rows, cached frames
     (4, 64, (8, 8), [300, 513], [7, 12]),
     (10, 128, (12, 20), [2000], [2]),
     (40, 128, (8, 8), [64], [3]),
+    (8, 64, (6, 12), [17, 0, 700, 1, 192, 65], [30, 8, 16, 201, 64, 90]),   # long and short streams together
+    (4, 128, (8, 8), [1000, 1, 30], [20, 70, 3]),
+    (2, 128, (8, 8), [1] * 30 + [40], [1] * 30 + [2]),         # spans of a few tiles, a wave each
+    (2, 64, (8, 8), [5, 9], [30, 31]),
 ]
 
 
