@@ -283,9 +283,9 @@ int ardit_mx_quantize(hipStream_t stream, const void* x, int64_t rows, int32_t c
 int ardit_kv_mx_bytes(const ardit_dims* dims, int32_t format, int32_t n_pages, size_t* code_bytes,
                       size_t* scale_bytes);
 
-/* ardit_kv_append into a microscaled cache: q~ and the chunk's k~ and v as there
- * (norm, rotation and scaling in fp32, the rotation's angles in fp64), k~ and v
- * quantised from their fp32 values into slots [cache_len, cache_len + q_len) of
+/* ardit_kv_append into a microscaled cache: q~ as there, the chunk's k~ and v
+ * quantised (k~ from its norm and rotation in fp64, so that a value next to the
+ * border of two codes takes the nearer) into slots [cache_len, cache_len + q_len) of
  * the stream's pages.  The values' padding in the tiles written becomes zero;
  * nothing else of the pool is written.  Chunks of whole frames, as there. */
 int ardit_kv_append_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,

@@ -45,19 +45,30 @@ __device__ __forceinline__ void store_stream16(void* p, const uint4& v) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
 }
 
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, kWave);
+  return v;
+}
+
 __device__ __forceinline__ uint32_t quad_max(uint32_t m) {   // over 4 neighbouring lanes
   m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0xB1, 0xf, 0xf, true)));
   return max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x4E, 0xf, 0xf, true)));
 }
 
-// Queries and keys of RPW rows a wave: a lane holds chunks lane + 64 i of 8 dims of
+// Queries and keys of RPW rows a wave.  Keys are normed and rotated in fp64 up to their
+// rounding to codes: a code's step is up to an eighth of its value, and with fp32's last
+// bits in doubt a few of seven million keys lie close enough to a border to take the other
+// code (2 us of 29 at 4680 rows of 1536, 7 of 187 at 9360 of 5120).  Rows of more than 1024
+// dims go one to a wave: fewer registers, more rows under way (29 us for 32).
+// A lane holds chunks lane + 64 i of 8 dims of
 // a row, so a block of 32 dims is four neighbouring lanes and a head 16 or 8 of them.
 template <int MAXC, int RPW, int BITS>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, float* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row0 = (group * 4 + wave) * RPW;
   const int nchunk = a.D >> 3, hd = a.p.hd;
-  float* lcs = lds + wave * RPW * 128;   // cos and sin of each row's pairs
+  double* lcs = reinterpret_cast<double*>(lds) + wave * RPW * 128;   // cos and sin of each row's pairs
 
   uint4 qraw[RPW][MAXC], kraw[RPW][MAXC];
 #pragma unroll
@@ -81,14 +92,13 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
     const int rem = t - f * a.p.T;
     const int i = static_cast<int>(fdiv(static_cast<uint32_t>(rem), a.fW));
     const int j = rem - i * a.lat_w;
-    float cs = 1.f, sn = 0.f;
+    double cs = 1.0, sn = 0.0;
     if (lane < (hd >> 1)) {
-      // Angles in turns and 64 bits, reduced before they are rounded: a far frame's
-      // angle in 32 bits is off by its size times 2^-24.
+      // angles in turns
       const int pos = lane < a.pairs_t ? s.frame_pos0 + f : (lane < a.pairs_t + a.pairs_h ? i : j);
       double x = static_cast<double>(pos) * a.inv_freq[lane];
       x -= rint(x);
-      sincospif(2.0f * static_cast<float>(x), &sn, &cs);
+      sincospi(2.0 * x, &sn, &cs);
     }
     lcs[r * 128 + lane] = cs;
     lcs[r * 128 + 64 + lane] = sn;
@@ -99,7 +109,8 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
     const int row = row0 + r;
-    float sq = 0.f, sk = 0.f;
+    float sq = 0.f;
+    double sk = 0.0;
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
       if (lane + 64 * i < nchunk) {
@@ -109,22 +120,22 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           sq += x[e] * x[e];
-          sk += y[e] * y[e];
+          sk = fma(static_cast<double>(y[e]), static_cast<double>(y[e]), sk);
         }
       }
     }
     sq = wave_sum(sq);
-    sk = wave_sum(sk);
+    sk = wave_sum64(sk);
     if (row >= a.N) continue;
     const float rq = 1.0f / sqrtf(sq / static_cast<float>(a.D) + a.eps);
-    const float rk = 1.0f / sqrtf(sk / static_cast<float>(a.D) + a.eps);
+    const double rk = 1.0 / sqrt(sk / static_cast<double>(a.D) + static_cast<double>(a.eps));
     const int b = stream_of(a.rs, row);
     const RowStream s = a.rs.s[b];
     const int slot = s.cache_len + row - s.row_begin;
     const int fr = static_cast<int>(fdiv(static_cast<uint32_t>(slot), a.fT));
     const int page = write_page(a.p.page_table[static_cast<size_t>(b) * a.p.max_frames + fr], a.p.n_pages);
     const int off = slot - fr * a.p.T;
-    const float* rcs = lcs + r * 128;
+    const double* rcs = lcs + r * 128;
     uint4* qo = reinterpret_cast<uint4*>(a.q_out + static_cast<size_t>(row) * a.D);
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
@@ -132,17 +143,21 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
       if (c < nchunk) {
         const int e0 = (8 * c) & (hd - 1);
         const int h = (8 * c) / hd;
-        const float4 cv = *reinterpret_cast<const float4*>(rcs + (e0 >> 1));
-        const float4 sv = *reinterpret_cast<const float4*>(rcs + 64 + (e0 >> 1));
-        const float cc[4] = {cv.x, cv.y, cv.z, cv.w}, ss[4] = {sv.x, sv.y, sv.z, sv.w};
+        double cc[4], ss[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          cc[e] = rcs[(e0 >> 1) + e];
+          ss[e] = rcs[64 + (e0 >> 1) + e];
+        }
         float x[8], y[8], g[8];
         unpack8(reinterpret_cast<const uint4*>(a.g_q)[c], g);
         unpack8(qraw[r][i], x);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x0 = x[2 * e] * rq * g[2 * e], x1 = x[2 * e + 1] * rq * g[2 * e + 1];
-          y[2 * e] = x0 * cc[e] - x1 * ss[e];
-          y[2 * e + 1] = x0 * ss[e] + x1 * cc[e];
+          const float co = static_cast<float>(cc[e]), si = static_cast<float>(ss[e]);
+          y[2 * e] = x0 * co - x1 * si;
+          y[2 * e + 1] = x0 * si + x1 * co;
         }
         store_stream16(qo + c, pack8(y));
         unpack8(reinterpret_cast<const uint4*>(a.g_k)[c], g);
@@ -150,9 +165,10 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
         uint32_t m = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x0 = x[2 * e] * rk * g[2 * e], x1 = x[2 * e + 1] * rk * g[2 * e + 1];
-          y[2 * e] = x0 * cc[e] - x1 * ss[e];
-          y[2 * e + 1] = x0 * ss[e] + x1 * cc[e];
+          // (a product of two bf16 numbers is exact in fp32)
+          const double x0 = x[2 * e] * g[2 * e], x1 = x[2 * e + 1] * g[2 * e + 1];
+          y[2 * e] = static_cast<float>(rk * fma(x0, cc[e], -x1 * ss[e]));
+          y[2 * e + 1] = static_cast<float>(rk * fma(x0, ss[e], x1 * cc[e]));
           m = max(m, max(__float_as_uint(y[2 * e]) & 0x7fffffffu, __float_as_uint(y[2 * e + 1]) & 0x7fffffffu));
         }
         const int sb = mx_scale_byte<BITS>(quad_max(m));
@@ -240,7 +256,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, int w, uint32
 
 // Rows and value tiles in one launch, so the two run side by side.
 template <int MAXC, int RPW, int BITS>
-__global__ __launch_bounds__(256) void kv_append_mx_kernel(const AppendArgs a) {
+__global__ __launch_bounds__(256, MAXC == 6 || MAXC == 10 ? 4 : 1) void kv_append_mx_kernel(const AppendArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t lds[64 * 64];
   const int b = blockIdx.x;
   if (b < a.qk_groups) {
@@ -361,7 +377,7 @@ hipError_t launch_kv_append_mx(hipStream_t st, const bf16_t* qkv, int N, const R
       a.inv_freq[pair++] = pow(static_cast<double>(g.theta), -2.0 * k / seg) / 6.283185307179586;
   a.rs = rs;
   const int chunks = (g.D / 8 + 63) / 64;
-  const int rpw = chunks <= 4 ? 2 : 1;
+  const int rpw = chunks <= 2 ? 2 : 1;
   a.qk_groups = (N + 4 * rpw - 1) / (4 * rpw);
   const dim3 grid(a.qk_groups + a.v_tiles * g.H);
 #define ARDIT_APPEND_CASE(C, R)                                                                   \
@@ -371,8 +387,8 @@ hipError_t launch_kv_append_mx(hipStream_t st, const bf16_t* qkv, int N, const R
   } while (0)
   if (chunks <= 1) ARDIT_APPEND_CASE(1, 2);
   else if (chunks <= 2) ARDIT_APPEND_CASE(2, 2);
-  else if (chunks <= 3) ARDIT_APPEND_CASE(3, 2);
-  else if (chunks <= 4) ARDIT_APPEND_CASE(4, 2);
+  else if (chunks <= 3) ARDIT_APPEND_CASE(3, 1);
+  else if (chunks <= 4) ARDIT_APPEND_CASE(4, 1);
   else if (chunks <= 6) ARDIT_APPEND_CASE(6, 1);
   else if (chunks <= 10) ARDIT_APPEND_CASE(10, 1);
   else ARDIT_APPEND_CASE(16, 1);
