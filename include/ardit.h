@@ -369,6 +369,15 @@ int ardit_stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batc
                     const void* const* ctx_k, const void* const* ctx_v,
                     const ardit_block_weights* w, void* out, void* ws, size_t ws_bytes);
 
+/* ardit_stack_fwd over microscaled caches, one per layer (host array): keys and
+ * values are quantised as they are appended, and attended to as quantised, the
+ * chunk's own too.  Streams bf16 and dense, as for ardit_attn_fwd_mx.  A block is a
+ * stack of one layer. */
+int ardit_stack_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                       int32_t n_layers, const void* x, const ardit_kv_mx* kv, const float* mod,
+                       const void* const* ctx_k, const void* const* ctx_v,
+                       const ardit_block_weights* w, void* out, void* ws, size_t ws_bytes);
+
 /* Page table of one stream under a sink + sliding-window cache (paper,
  * Section 2.1: the cache keeps a few sink chunks plus the most recent W
  * chunks; Sections 3.2 and 4.4: frame pages behind a logical table).  While
@@ -428,6 +437,16 @@ int ardit_chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit
                          const ardit_kv_paged* kv, const ardit_time_weights* tw,
                          const void* const* ctx_k, const void* const* ctx_v,
                          const ardit_block_weights* w, void* x0_out, void* ws, size_t ws_bytes);
+
+/* ardit_chunk_generate over microscaled caches, one per layer (host array); the
+ * commit pass leaves the clean chunk's quantised keys and values in them. */
+int ardit_chunk_generate_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                            int32_t n_layers, const int32_t* n_steps, const float* t_host,
+                            int32_t t_ld, const void* x_init, const void* noise,
+                            const ardit_kv_mx* kv, const ardit_time_weights* tw,
+                            const void* const* ctx_k, const void* const* ctx_v,
+                            const ardit_block_weights* w, void* x0_out, void* ws,
+                            size_t ws_bytes);
 
 /* Kernel timing.  ardit_timing_enable(mask) turns on HIP events recorded on
  * the launch stream around each launch of the kinds in mask: bit 0 (1) the

@@ -131,11 +131,18 @@ _SIGS = {
     "ardit_stack_fwd": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _vp,
                                   _P(ardit_kv_paged), _vp, _P(_vp), _P(_vp),
                                   _P(ardit_block_weights), _vp, _vp, _sz]),
+    "ardit_stack_fwd_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _vp,
+                                     _P(ardit_kv_mx), _vp, _P(_vp), _P(_vp),
+                                     _P(ardit_block_weights), _vp, _vp, _sz]),
     "ardit_window_pages": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _P(_i32), _i32, _P(_i32)]),
     "ardit_chunk_generate": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _P(_i32),
                                        _P(C.c_float), _i32, _vp, _vp, _P(ardit_kv_paged),
                                        _P(ardit_time_weights), _P(_vp), _P(_vp),
                                        _P(ardit_block_weights), _vp, _vp, _sz]),
+    "ardit_chunk_generate_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _P(_i32),
+                                          _P(C.c_float), _i32, _vp, _vp, _P(ardit_kv_mx),
+                                          _P(ardit_time_weights), _P(_vp), _P(_vp),
+                                          _P(ardit_block_weights), _vp, _vp, _sz]),
     "ardit_pareto_frontier": (C.c_int, [_i32, _P(ardit_fidelity), _P(_i32), _P(_i32),
                                         _P(C.c_double)]),
     "ardit_bmpr_select": (C.c_int, [_i32, _P(ardit_fidelity), _i32, _P(_i32), C.c_double,
@@ -362,16 +369,29 @@ def ardit_block_fwd_varlen(stream, dims, batch: Batch, x, kv: ardit_kv_paged, mo
            "ardit_block_fwd_varlen")
 
 
-def ardit_stack_fwd(stream, dims, batch: Batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, out, ws,
-                    ws_bytes):
+def _stack(name, kv_type, stream, dims, batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, out, ws,
+           ws_bytes):
     L = len(kvs)
-    kv_arr = (ardit_kv_paged * L)(*kvs)
+    kv_arr = (kv_type * L)(*kvs)
     w_arr = (ardit_block_weights * L)(*ws_list)
     ck = (C.c_void_p * L)(*[_ptr(t) for t in ctx_ks])
     cv = (C.c_void_p * L)(*[_ptr(t) for t in ctx_vs])
-    _check(_lib.ardit_stack_fwd(_stream(stream), C.byref(dims), C.byref(batch.struct), L, _ptr(x),
-                                kv_arr, _ptr(mod), ck, cv, w_arr, _ptr(out), _ptr(ws),
-                                int(ws_bytes)), "ardit_stack_fwd")
+    _check(getattr(_lib, name)(_stream(stream), C.byref(dims), C.byref(batch.struct), L, _ptr(x),
+                               kv_arr, _ptr(mod), ck, cv, w_arr, _ptr(out), _ptr(ws),
+                               int(ws_bytes)), name)
+
+
+def ardit_stack_fwd(stream, dims, batch: Batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, out, ws,
+                    ws_bytes):
+    _stack("ardit_stack_fwd", ardit_kv_paged, stream, dims, batch, x, kvs, mod, ctx_ks, ctx_vs,
+           ws_list, out, ws, ws_bytes)
+
+
+def ardit_stack_fwd_mx(stream, dims, batch: Batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, out, ws,
+                       ws_bytes):
+    """kvs: ardit_kv_mx per layer."""
+    _stack("ardit_stack_fwd_mx", ardit_kv_mx, stream, dims, batch, x, kvs, mod, ctx_ks, ctx_vs,
+           ws_list, out, ws, ws_bytes)
 
 
 def ardit_window_pages(chunk, sink, window, frames_per_chunk, page_base=0, max_frames=None):
@@ -387,9 +407,8 @@ def ardit_window_pages(chunk, sink, window, frames_per_chunk, page_base=0, max_f
     return [table[i] for i in range(n)], cached.value
 
 
-def ardit_chunk_generate(stream, dims, batch: Batch, n_steps, timesteps, x_init, noise, kvs,
-                         tw: ardit_time_weights, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes):
-    """timesteps: per stream, the list of its n_steps[b] timesteps."""
+def _chunk(name, kv_type, stream, dims, batch, n_steps, timesteps, x_init, noise, kvs, tw, ctx_ks,
+           ctx_vs, ws_list, x0_out, ws, ws_bytes):
     L = len(kvs)
     B = len(n_steps)
     t_ld = max(1, max(int(s) for s in n_steps))
@@ -398,14 +417,27 @@ def ardit_chunk_generate(stream, dims, batch: Batch, n_steps, timesteps, x_init,
         for i, v in enumerate(ts):
             t[b * t_ld + i] = float(v)
     ns = (C.c_int32 * B)(*[int(v) for v in n_steps])
-    kv_arr = (ardit_kv_paged * L)(*kvs)
+    kv_arr = (kv_type * L)(*kvs)
     w_arr = (ardit_block_weights * L)(*ws_list)
     ck = (C.c_void_p * L)(*[_ptr(x) for x in ctx_ks])
     cv = (C.c_void_p * L)(*[_ptr(x) for x in ctx_vs])
-    _check(_lib.ardit_chunk_generate(_stream(stream), C.byref(dims), C.byref(batch.struct), L, ns,
-                                     t, t_ld, _ptr(x_init), _ptr(noise), kv_arr, C.byref(tw), ck,
-                                     cv, w_arr, _ptr(x0_out), _ptr(ws), int(ws_bytes)),
-           "ardit_chunk_generate")
+    _check(getattr(_lib, name)(_stream(stream), C.byref(dims), C.byref(batch.struct), L, ns, t,
+                               t_ld, _ptr(x_init), _ptr(noise), kv_arr, C.byref(tw), ck, cv, w_arr,
+                               _ptr(x0_out), _ptr(ws), int(ws_bytes)), name)
+
+
+def ardit_chunk_generate(stream, dims, batch: Batch, n_steps, timesteps, x_init, noise, kvs,
+                         tw: ardit_time_weights, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes):
+    """timesteps: per stream, the list of its n_steps[b] timesteps."""
+    _chunk("ardit_chunk_generate", ardit_kv_paged, stream, dims, batch, n_steps, timesteps, x_init,
+           noise, kvs, tw, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes)
+
+
+def ardit_chunk_generate_mx(stream, dims, batch: Batch, n_steps, timesteps, x_init, noise, kvs,
+                            tw: ardit_time_weights, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes):
+    """kvs: ardit_kv_mx per layer; the rest as for ardit_chunk_generate."""
+    _chunk("ardit_chunk_generate_mx", ardit_kv_mx, stream, dims, batch, n_steps, timesteps, x_init,
+           noise, kvs, tw, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes)
 
 
 TIME_ATTENTION, TIME_GEMM, TIME_ELEMENTWISE = 0, 1, 2

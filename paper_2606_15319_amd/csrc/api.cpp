@@ -260,7 +260,7 @@ int check_format(int32_t format) {
   return ARDIT_OK;
 }
 
-int check_kv_mx(const ardit_dims* d, const ardit_batch* b, const ardit_kv_mx* kv) {
+int check_kv(const ardit_dims* d, const ardit_batch* b, const ardit_kv_mx* kv) {
   if (!kv) return fail(ARDIT_EINVAL, "kv is NULL");
   if (!kv->k_codes || !kv->k_scales || !kv->v_codes || !kv->v_scales || !kv->page_table)
     return fail(ARDIT_EINVAL, "kv pointers must be non-NULL");
@@ -757,11 +757,41 @@ int attention_mx(hipStream_t st, const ardit_dims* d, const ardit_batch* b, cons
   return ARDIT_OK;
 }
 
+// The two steps of a block that touch its cache, for either kind of cache.
+int block_append(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const bf16_t* qkv,
+                 const ardit_block_weights* w, const ardit_kv_paged* kv, bf16_t* q) {
+  RopeGeom rg{d->dim, d->n_heads, d->head_dim, tokens_per_frame(d), d->lat_w, kv->max_frames,
+              kv->n_pages, d->eps, d->rope_theta};
+  ARDIT_TIMED(kTimeElem,
+              launch_kv_append(st, qkv, static_cast<int>(sum_q(b)), rg,
+                               static_cast<const bf16_t*>(w->g_q), static_cast<const bf16_t*>(w->g_k), q,
+                               static_cast<bf16_t*>(kv->k_pages),
+                               static_cast<bf16_t*>(kv->v_pages), kv->page_table, q_streams(b)),
+              "qk_norm_rope / kv append");
+  return ARDIT_OK;
+}
+int block_append(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const bf16_t* qkv,
+                 const ardit_block_weights* w, const ardit_kv_mx* kv, bf16_t* q) {
+  return append_mx(st, d, b, qkv, w->g_q, w->g_k, kv, q);
+}
+int block_attention(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* q,
+                    const ardit_kv_paged* kv, void* o, void* ws, const Ws& L) {
+  return self_attention(st, d, b, q, kv, o, ws, L);
+}
+int block_attention(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* q,
+                    const ardit_kv_mx* kv, void* o, void* ws, const Ws& L) {
+  return attention_mx(st, d, b, q, kv, 0, o, ws, L);
+}
+// what a kind of cache asks of the batch's streams
+int check_streams(const ardit_dims* d, const ardit_batch* b, const ardit_kv_paged*) { return check_sparse(d, b); }
+int check_streams(const ardit_dims*, const ardit_batch* b, const ardit_kv_mx*) { return check_mx_streams(b); }
+
 // the block chain on validated arguments
 // (kv_only: stop once the chunk's keys and values are in the pages; out is
 // not written)
+template <typename KV>
 int block_chain(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* xin,
-                const ardit_kv_paged* kv, const float* mod, const void* ctx_k, const void* ctx_v,
+                const KV* kv, const float* mod, const void* ctx_k, const void* ctx_v,
                 const ardit_block_weights* w, void* out, void* ws, const Ws& L,
                 bool kv_only = false) {
   const int N = static_cast<int>(sum_q(b));
@@ -777,7 +807,6 @@ int block_chain(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const
   bf16_t* u = at<bf16_t>(ws, L.u);
   bf16_t* y = static_cast<bf16_t*>(out);
   const float* mt = w->mod_table;
-  const RowStreams rs = q_streams(b);
   auto B16 = [](const void* p) { return static_cast<const bf16_t*>(p); };
 
   // adaLN RMSNorm #1 and the QKV projection
@@ -788,16 +817,10 @@ int block_chain(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const
   ARDIT_TIMED(kTimeGemm, launch_gemm(st, kEpiBias, h, D, B16(w->w_qkv), D, qkv, 3 * D, N, 3 * D, D, e),
               "qkv gemm");
   // QK-norm, 3D RoPE, append k~ and v to the pages
-  RopeGeom rg{D, H, hd, tokens_per_frame(d), d->lat_w, kv->max_frames, kv->n_pages, d->eps,
-              d->rope_theta};
-  ARDIT_TIMED(kTimeElem,
-              launch_kv_append(st, qkv, N, rg, B16(w->g_q), B16(w->g_k), q,
-                               static_cast<bf16_t*>(kv->k_pages),
-                               static_cast<bf16_t*>(kv->v_pages), kv->page_table, rs),
-              "qk_norm_rope / kv append");
+  ARDIT_TRY(block_append(st, d, b, qkv, w, kv, q));
   if (kv_only) return ARDIT_OK;
   // self-attention over [cache | chunk]
-  ARDIT_TRY(self_attention(st, d, b, q, kv, o, ws, L));
+  ARDIT_TRY(block_attention(st, d, b, q, kv, o, ws, L));
   // x1 = x + gate1 * (o W_o^T + b_o)
   e = GemmEpiArgs();
   e.bias = B16(w->b_o);
@@ -885,13 +908,14 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   return na && nb && x < y + nb && y < x + na;
 }
 
+template <typename KV>
 int check_block_args(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* x,
-                     const ardit_kv_paged* kv, const float* mod, const void* ctx_k,
+                     const KV* kv, const float* mod, const void* ctx_k,
                      const void* ctx_v, const ardit_block_weights* w, const void* out) {
   ARDIT_TRY(check_dims(d));
   ARDIT_TRY(check_batch(d, b, kUseQ | kUseCache | kUsePos | kUseCtx | kChunkQ));
   ARDIT_TRY(check_kv(d, b, kv));
-  ARDIT_TRY(check_sparse(d, b));
+  ARDIT_TRY(check_streams(d, b, kv));
   ARDIT_TRY(check_ptr(x, "x"));
   ARDIT_TRY(check_ptr(out, "out"));
   ARDIT_TRY(check_ptr(mod, "mod"));
@@ -899,6 +923,116 @@ int check_block_args(hipStream_t st, const ardit_dims* d, const ardit_batch* b, 
   ARDIT_TRY(check_ptr(ctx_v, "ctx_v"));
   ARDIT_TRY(check_block_weights(w, false));
   return check_pages(st, d, b, kv, true);
+}
+
+// n_layers blocks over either kind of cache
+template <typename KV>
+int stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch, int32_t n_layers,
+              const void* x, const KV* kv, const float* mod, const void* const* ctx_k,
+              const void* const* ctx_v, const ardit_block_weights* w, void* out, void* ws,
+              size_t ws_bytes) {
+  if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
+  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
+  for (int l = 0; l < n_layers; ++l)
+    ARDIT_TRY(check_block_args(stream, dims, batch, x, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l], out));
+  if (x == out) return fail(ARDIT_EINVAL, "stack input and output must differ");
+  Ws L;
+  ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
+  // layer 0 reads x and writes out; later layers update out in place (a
+  // layer reads its input only before it writes its output)
+  for (int l = 0; l < n_layers; ++l)
+    ARDIT_TRY(block_chain(stream, dims, batch, l == 0 ? x : out, &kv[l], mod, ctx_k[l], ctx_v[l],
+                          &w[l], out, ws, L));
+  return ARDIT_OK;
+}
+
+// a chunk's denoising and commit passes over either kind of cache
+template <typename KV>
+int chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                   int32_t n_layers, const int32_t* n_steps, const float* t_host, int32_t t_ld,
+                   const void* x_init, const void* noise, const KV* kv,
+                   const ardit_time_weights* tw, const void* const* ctx_k,
+                   const void* const* ctx_v, const ardit_block_weights* w, void* x0_out, void* ws,
+                   size_t ws_bytes) {
+  ARDIT_TRY(check_dims(dims));
+  ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache | kUsePos | kUseCtx | kChunkQ));
+  if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
+  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
+  if (!n_steps || !t_host) return fail(ARDIT_EINVAL, "n_steps and t_host must be non-NULL");
+  const int B = batch->n_streams;
+  const int S0 = n_steps[0];
+  for (int b = 0; b < B; ++b) {
+    if (n_steps[b] < 1 || n_steps[b] > ARDIT_MAX_STEPS)
+      return fail(ARDIT_EINVAL, "n_steps[%d] = %d not in [1, %d]", b, n_steps[b],
+                  ARDIT_MAX_STEPS);
+    if (b > 0 && n_steps[b] > n_steps[b - 1])
+      return fail(ARDIT_EINVAL, "n_steps must be non-increasing along the batch (stream %d)", b);
+  }
+  if (t_ld < S0) return fail(ARDIT_EINVAL, "t_ld %d below n_steps[0] = %d", t_ld, S0);
+  for (int b = 0; b < B; ++b)
+    for (int i = 0; i < n_steps[b]; ++i) {
+      const float t = t_host[static_cast<size_t>(b) * t_ld + i];
+      if (!(t >= 0.f && t <= 1000.f))
+        return fail(ARDIT_EINVAL, "timestep %g of stream %d step %d not in [0, 1000]",
+                    static_cast<double>(t), b, i);
+    }
+  ARDIT_TRY(check_time_weights(tw));
+  ARDIT_TRY(check_ptr(x_init, "x_init"));
+  ARDIT_TRY(check_ptr(x0_out, "x0_out"));
+  if (S0 > 1) ARDIT_TRY(check_ptr(noise, "noise"));
+  Ws L;
+  ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
+  float* mod = at<float>(ws, L.gmod);
+  bf16_t* vel = at<bf16_t>(ws, L.gv);
+  for (int l = 0; l < n_layers; ++l)
+    ARDIT_TRY(check_block_args(stream, dims, batch, x_init, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l],
+                               vel));
+  const int64_t N = sum_q(batch);
+  const int D = dims->dim;
+  const size_t xbytes = 2 * static_cast<size_t>(N) * D;
+  if (overlaps(x0_out, xbytes, x_init, xbytes) ||
+      (S0 > 1 && overlaps(x0_out, xbytes, noise, xbytes * (S0 - 1))) ||
+      overlaps(x0_out, xbytes, ws, L.total))
+    return fail(ARDIT_EINVAL, "x0_out overlaps x_init, noise or the workspace");
+
+  const int Lq = chunk_tokens(dims);
+  // pass i runs the streams with n_steps >= i (a prefix): denoising step i of
+  // those with n_steps > i, the commit pass (t = 0) of those with n_steps == i
+  for (int i = 0; i <= S0; ++i) {
+    int active = 0, denoise = 0;
+    float t[ARDIT_MAX_STREAMS];
+    SamplerArgs sa;
+    for (int b = 0; b < B; ++b) {
+      if (n_steps[b] >= i) active = b + 1;
+      if (n_steps[b] > i) denoise = b + 1;
+      const bool step = i < n_steps[b];
+      t[b] = step ? t_host[static_cast<size_t>(b) * t_ld + i] : 0.f;
+      sa.tau[b] = static_cast<float>(static_cast<double>(t[b]) / 1000.0);
+      sa.tau_next[b] = step && i + 1 < n_steps[b]
+          ? static_cast<float>(static_cast<double>(t_host[static_cast<size_t>(b) * t_ld + i + 1]) /
+                               1000.0)
+          : -1.f;
+    }
+    ardit_batch sb = *batch;
+    sb.n_streams = active;
+    ARDIT_TRY(time_mod_chain(stream, dims, active, t, tw, mod, ws, L));
+    const void* xin = i == 0 ? x_init : x0_out;
+    // a pass that only commits needs no output of its last layer
+    const bool commit_only = denoise == 0;
+    for (int l = 0; l < n_layers; ++l)
+      ARDIT_TRY(block_chain(stream, dims, &sb, l == 0 ? xin : vel, &kv[l], mod, ctx_k[l],
+                            ctx_v[l], &w[l], vel, ws, L, commit_only && l == n_layers - 1));
+    if (denoise > 0) {
+      sa.rows = denoise * Lq;
+      sa.rows_per_stream = Lq;
+      sa.vec_per_row = D / 8;
+      const bf16_t* eps = i + 1 < S0 ? static_cast<const bf16_t*>(noise) + i * N * D : nullptr;
+      ARDIT_HIP(launch_sampler(stream, static_cast<const bf16_t*>(xin), vel, eps,
+                               static_cast<bf16_t*>(x0_out), sa),
+                "sampler");
+    }
+  }
+  return ARDIT_OK;
 }
 
 // ------------------------------------------------ allocation-free attention
@@ -1167,7 +1301,7 @@ int ardit_kv_append_mx(hipStream_t stream, const ardit_dims* dims, const ardit_b
                        void* q_out) try {
   ARDIT_TRY(check_dims(dims));
   ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache | kUsePos | kChunkQ));
-  ARDIT_TRY(check_kv_mx(dims, batch, kv));
+  ARDIT_TRY(check_kv(dims, batch, kv));
   ARDIT_TRY(check_ptr(qkv, "qkv"));
   ARDIT_TRY(check_ptr(g_q, "g_q"));
   ARDIT_TRY(check_ptr(g_k, "g_k"));
@@ -1182,7 +1316,7 @@ int ardit_kv_read_mx(hipStream_t stream, const ardit_dims* dims, const ardit_bat
                      const ardit_kv_mx* src, const ardit_kv_paged* dst) try {
   ARDIT_TRY(check_dims(dims));
   ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache));
-  ARDIT_TRY(check_kv_mx(dims, batch, src));
+  ARDIT_TRY(check_kv(dims, batch, src));
   ARDIT_TRY(check_kv(dims, batch, dst));
   ARDIT_TRY(check_pages(stream, dims, batch, src, false, true));
   ARDIT_TRY(check_pages(stream, dims, batch, dst, true, true));
@@ -1200,7 +1334,7 @@ int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_ba
                       size_t ws_bytes) try {
   ARDIT_TRY(check_dims(dims));
   ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache));
-  ARDIT_TRY(check_kv_mx(dims, batch, kv));
+  ARDIT_TRY(check_kv(dims, batch, kv));
   ARDIT_TRY(check_mx_streams(batch));
   if (shared_frames < 0) return fail(ARDIT_EINVAL, "shared_frames %d is negative", shared_frames);
   for (int i = 0; i < batch->n_streams; ++i)
@@ -1292,19 +1426,16 @@ int ardit_stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batc
                     int32_t n_layers, const void* x, const ardit_kv_paged* kv, const float* mod,
                     const void* const* ctx_k, const void* const* ctx_v,
                     const ardit_block_weights* w, void* out, void* ws, size_t ws_bytes) try {
-  if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
-  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
-  for (int l = 0; l < n_layers; ++l)
-    ARDIT_TRY(check_block_args(stream, dims, batch, x, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l], out));
-  if (x == out) return fail(ARDIT_EINVAL, "stack input and output must differ");
-  Ws L;
-  ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
-  // layer 0 reads x and writes out; later layers update out in place (a
-  // layer reads its input only before it writes its output)
-  for (int l = 0; l < n_layers; ++l)
-    ARDIT_TRY(block_chain(stream, dims, batch, l == 0 ? x : out, &kv[l], mod, ctx_k[l], ctx_v[l],
-                          &w[l], out, ws, L));
-  return ARDIT_OK;
+  return stack_fwd(stream, dims, batch, n_layers, x, kv, mod, ctx_k, ctx_v, w, out, ws, ws_bytes);
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_stack_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                       int32_t n_layers, const void* x, const ardit_kv_mx* kv, const float* mod,
+                       const void* const* ctx_k, const void* const* ctx_v,
+                       const ardit_block_weights* w, void* out, void* ws, size_t ws_bytes) try {
+  return stack_fwd(stream, dims, batch, n_layers, x, kv, mod, ctx_k, ctx_v, w, out, ws, ws_bytes);
 } catch (...) {
   return host_failure();
 }
@@ -1349,85 +1480,20 @@ int ardit_chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit
                          const ardit_kv_paged* kv, const ardit_time_weights* tw,
                          const void* const* ctx_k, const void* const* ctx_v,
                          const ardit_block_weights* w, void* x0_out, void* ws, size_t ws_bytes) try {
-  ARDIT_TRY(check_dims(dims));
-  ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache | kUsePos | kUseCtx | kChunkQ));
-  if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
-  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
-  if (!n_steps || !t_host) return fail(ARDIT_EINVAL, "n_steps and t_host must be non-NULL");
-  const int B = batch->n_streams;
-  const int S0 = n_steps[0];
-  for (int b = 0; b < B; ++b) {
-    if (n_steps[b] < 1 || n_steps[b] > ARDIT_MAX_STEPS)
-      return fail(ARDIT_EINVAL, "n_steps[%d] = %d not in [1, %d]", b, n_steps[b],
-                  ARDIT_MAX_STEPS);
-    if (b > 0 && n_steps[b] > n_steps[b - 1])
-      return fail(ARDIT_EINVAL, "n_steps must be non-increasing along the batch (stream %d)", b);
-  }
-  if (t_ld < S0) return fail(ARDIT_EINVAL, "t_ld %d below n_steps[0] = %d", t_ld, S0);
-  for (int b = 0; b < B; ++b)
-    for (int i = 0; i < n_steps[b]; ++i) {
-      const float t = t_host[static_cast<size_t>(b) * t_ld + i];
-      if (!(t >= 0.f && t <= 1000.f))
-        return fail(ARDIT_EINVAL, "timestep %g of stream %d step %d not in [0, 1000]",
-                    static_cast<double>(t), b, i);
-    }
-  ARDIT_TRY(check_time_weights(tw));
-  ARDIT_TRY(check_ptr(x_init, "x_init"));
-  ARDIT_TRY(check_ptr(x0_out, "x0_out"));
-  if (S0 > 1) ARDIT_TRY(check_ptr(noise, "noise"));
-  Ws L;
-  ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
-  float* mod = at<float>(ws, L.gmod);
-  bf16_t* vel = at<bf16_t>(ws, L.gv);
-  for (int l = 0; l < n_layers; ++l)
-    ARDIT_TRY(check_block_args(stream, dims, batch, x_init, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l],
-                               vel));
-  const int64_t N = sum_q(batch);
-  const int D = dims->dim;
-  const size_t xbytes = 2 * static_cast<size_t>(N) * D;
-  if (overlaps(x0_out, xbytes, x_init, xbytes) ||
-      (S0 > 1 && overlaps(x0_out, xbytes, noise, xbytes * (S0 - 1))) ||
-      overlaps(x0_out, xbytes, ws, L.total))
-    return fail(ARDIT_EINVAL, "x0_out overlaps x_init, noise or the workspace");
+  return chunk_generate(stream, dims, batch, n_layers, n_steps, t_host, t_ld, x_init, noise, kv, tw,
+                        ctx_k, ctx_v, w, x0_out, ws, ws_bytes);
+} catch (...) {
+  return host_failure();
+}
 
-  const int Lq = chunk_tokens(dims);
-  // pass i runs the streams with n_steps >= i (a prefix): denoising step i of
-  // those with n_steps > i, the commit pass (t = 0) of those with n_steps == i
-  for (int i = 0; i <= S0; ++i) {
-    int active = 0, denoise = 0;
-    float t[ARDIT_MAX_STREAMS];
-    SamplerArgs sa;
-    for (int b = 0; b < B; ++b) {
-      if (n_steps[b] >= i) active = b + 1;
-      if (n_steps[b] > i) denoise = b + 1;
-      const bool step = i < n_steps[b];
-      t[b] = step ? t_host[static_cast<size_t>(b) * t_ld + i] : 0.f;
-      sa.tau[b] = static_cast<float>(static_cast<double>(t[b]) / 1000.0);
-      sa.tau_next[b] = step && i + 1 < n_steps[b]
-          ? static_cast<float>(static_cast<double>(t_host[static_cast<size_t>(b) * t_ld + i + 1]) /
-                               1000.0)
-          : -1.f;
-    }
-    ardit_batch sb = *batch;
-    sb.n_streams = active;
-    ARDIT_TRY(time_mod_chain(stream, dims, active, t, tw, mod, ws, L));
-    const void* xin = i == 0 ? x_init : x0_out;
-    // a pass that only commits needs no output of its last layer
-    const bool commit_only = denoise == 0;
-    for (int l = 0; l < n_layers; ++l)
-      ARDIT_TRY(block_chain(stream, dims, &sb, l == 0 ? xin : vel, &kv[l], mod, ctx_k[l],
-                            ctx_v[l], &w[l], vel, ws, L, commit_only && l == n_layers - 1));
-    if (denoise > 0) {
-      sa.rows = denoise * Lq;
-      sa.rows_per_stream = Lq;
-      sa.vec_per_row = D / 8;
-      const bf16_t* eps = i + 1 < S0 ? static_cast<const bf16_t*>(noise) + i * N * D : nullptr;
-      ARDIT_HIP(launch_sampler(stream, static_cast<const bf16_t*>(xin), vel, eps,
-                               static_cast<bf16_t*>(x0_out), sa),
-                "sampler");
-    }
-  }
-  return ARDIT_OK;
+int ardit_chunk_generate_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                            int32_t n_layers, const int32_t* n_steps, const float* t_host,
+                            int32_t t_ld, const void* x_init, const void* noise,
+                            const ardit_kv_mx* kv, const ardit_time_weights* tw,
+                            const void* const* ctx_k, const void* const* ctx_v,
+                            const ardit_block_weights* w, void* x0_out, void* ws, size_t ws_bytes) try {
+  return chunk_generate(stream, dims, batch, n_layers, n_steps, t_host, t_ld, x_init, noise, kv, tw,
+                        ctx_k, ctx_v, w, x0_out, ws, ws_bytes);
 } catch (...) {
   return host_failure();
 }

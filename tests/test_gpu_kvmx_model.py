@@ -1,0 +1,123 @@
+"""The model path over microscaled caches: stacks and whole chunks."""
+import numpy as np
+import pytest
+
+import oracle as O
+from harness import BlockRun, dev_bf16, host_bits, host_f32, parity
+from oracle import ardit_ref as R
+from oracle import mxkv_ref as M
+from test_gpu_chunk import LQ, SH, Model, _sampler_bits
+from test_gpu_kvmx import Pool
+from workloads import WORKLOADS, BlockShape, bits_to_f32, normal_bf16
+from workloads.gen import Workload
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A(gpu):
+    from paper_2606_15319_amd import ardit
+    return ardit
+
+
+def _sync():
+    import torch
+    torch.cuda.synchronize()
+
+
+def _pool(A, shape, bits, lens, cached, seed):
+    """A pool of streams of `lens` tokens whose first `cached` tokens are drawn."""
+    p = Pool(A, shape.n_heads, shape.head_dim, (shape.lat_h, shape.lat_w), shape.frames, bits, lens, seed=seed)
+    ids = [list(i) for i in p.ids]
+    p.ids = [i[:c // p.T] for i, c in zip(ids, cached)]
+    p.fill(cached, seed)
+    p.ids = ids
+    return p
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("name", ["tiny", "wide"])
+def test_a_block_over_a_microscaled_cache(A, bits, name):
+    """One layer: the block of the keys and values that its pages end up holding, and pages
+    that hold the chunk's own to within their formats' rounding."""
+    if name == "tiny":
+        wl = WORKLOADS["tiny"]
+    else:
+        wl = Workload(wid=77, name="wide", cache_chunks=(2, 0, 1), frame_pos0=(4, 0, 9), ctx_len=24,
+                      shape=BlockShape(dim=256, n_heads=2, head_dim=128, ffn_dim=512, frames=2, lat_h=6, lat_w=12))
+    run = BlockRun(wl, A)
+    sh, c = run.shape, run.case
+    L = sh.chunk_tokens
+    pool = _pool(A, sh, bits, [n + L for n in c.cache_len], c.cache_len, 5)
+    wts = A.block_weights(run.w_dev)
+    A.ardit_time_mod(None, run.dims, c.t, A.time_weights(run.tw_dev), run.mod, run.ws, run.ws_bytes)
+    A.ardit_ctx_kv(None, run.dims, run.batch, run.ctx, wts, run.ctx_k, run.ctx_v, run.ws, run.ws_bytes)
+    A.ardit_stack_fwd_mx(None, run.dims, run.batch, run.x, [pool.kv()], run.mod, [run.ctx_k], [run.ctx_v], [wts],
+                         run.out, run.ws, run.ws_bytes)
+    _sync()
+    pool.download()
+    out = host_f32(run.out).astype(np.float64)
+    for b in range(run.B):
+        pages = [pool.host.unpack(p) for p in pool.ids[b]]
+        k, v = (np.concatenate(z) for z in zip(*pages))
+        m_t = O.time_modulation(c.t[b], c.time_w, sh.dim)
+        mod = R._modulation(m_t, c.block_w)
+        where = O.chunk_positions(sh.frames, sh.lat_h, sh.lat_w, c.frame_pos0[b])
+        q, kn, vn = R._qkv_rope(c.x[b].astype(np.float64), mod, c.block_w, sh, where)
+        # the chunk's own: rounded to codes from projections stored in bf16 (2^-8 of a value; the rotation and the
+        # norm mix at most two of them with unit weights)
+        for f in range(sh.frames):
+            at = slice(f * pool.T, (f + 1) * pool.T)
+            for got, want, axis in ((k, kn, -1), (v, vn, 0)):
+                g = got[c.cache_len[b] + f * pool.T:][:pool.T]
+                noise = np.linalg.norm(M.rounded(want[at], bits, axis) - want[at])
+                assert np.linalg.norm(g - want[at]) <= 1.03 * noise + 2.0 ** -8 * np.linalg.norm(want[at])
+        kc, vc = O.context_kv(c.ctx[b], c.block_w, sh.eps)
+        o = O.attention(q, k, v).reshape(L, sh.dim)
+        ref = R._after_self_attention(c.x[b].astype(np.float64), o, mod, c.block_w, sh, kc, vc)["out"]
+        parity(out[b * L:(b + 1) * L], ref, f"{name} {bits} bits stream {b}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_a_chunk_equals_its_passes(A, bits):
+    """Streams of two steps and one: the call equals the passes composed by hand, x0 and every
+    byte of every layer's pages."""
+    import torch
+    n_layers, n_steps, ts = 2, [2, 1], [[1000.0, 500.0], [800.0]]
+    chunks = [2, 1]
+    m = Model(A, 91, n_layers, [20, 9])
+    lens, cached = [(c + 1) * LQ for c in chunks], [c * LQ for c in chunks]
+    pools = [[_pool(A, SH, bits, lens, cached, 30 + l) for l in range(n_layers)] for _ in range(2)]
+    batch = A.Batch([LQ] * 2, cached, [3 * c for c in chunks], m.ctx_lens)
+    ws, n = m.workspace(batch)
+    x = normal_bf16(m.rng, (2 * LQ, SH.dim))
+    noise = normal_bf16(m.rng, (1, 2 * LQ, SH.dim))
+    x_dev, noise_dev = dev_bf16(x), dev_bf16(noise)
+    x0 = torch.full((2 * LQ, SH.dim), float("nan"), dtype=torch.bfloat16, device="cuda")
+    A.ardit_chunk_generate_mx(None, m.dims, batch, n_steps, ts, x_dev, noise_dev, [p.kv() for p in pools[0]], m.tw,
+                              m.ctx_k, m.ctx_v, m.w, x0, ws, n)
+    _sync()
+
+    def one_pass(xb, t, streams):
+        sub = A.Batch([LQ] * streams, cached[:streams], [3 * c for c in chunks[:streams]], m.ctx_lens[:streams])
+        mod = torch.empty((streams, 6, SH.dim), dtype=torch.float32, device="cuda")
+        A.ardit_time_mod(None, m.dims, t, m.tw, mod, ws, n)
+        xd = dev_bf16(bits_to_f32(xb[:streams * LQ]))
+        v = torch.empty_like(xd)
+        A.ardit_stack_fwd_mx(None, m.dims, sub, xd, [p.kv() for p in pools[1]], mod, m.ctx_k, m.ctx_v, m.w, v, ws, n)
+        _sync()
+        return host_f32(v)
+
+    cur = host_bits(x_dev).copy()
+    xf = bits_to_f32(cur)
+    v = one_pass(cur, [1000.0, 800.0], 2)
+    cur[:LQ] = _sampler_bits(xf[:LQ], v[:LQ], 1.0, 0.5, noise[0, :LQ])
+    cur[LQ:] = _sampler_bits(xf[LQ:], v[LQ:], 0.8, None, None)
+    xf = bits_to_f32(cur)
+    v = one_pass(cur, [500.0, 0.0], 2)              # the second stream commits
+    cur[:LQ] = _sampler_bits(xf[:LQ], v[:LQ], 0.5, None, None)
+    one_pass(cur, [0.0], 1)
+    assert np.array_equal(host_bits(x0), cur)
+    for a, b in zip(*pools):
+        for s, t in zip(a.dev, b.dev):
+            assert np.array_equal(s.cpu().numpy(), t.cpu().numpy())

@@ -176,3 +176,43 @@ def test_attention_refusals():
     small = _dims(lat_h=4, lat_w=8)
     assert call(dims=small, batch=A.Batch([5], [1 << 30]), nbytes=1 << 40,
                 kv=_mx(max_frames=1 << 26)) == -3
+
+
+def _stack(batch=None, kv=None, dims=None, nbytes=1 << 40, x=FAKE, out=FAKE + 4096, mod=FAKE, ctx=FAKE):
+    d = dims or _dims()
+    w = A.block_weights({k: FAKE for k in A._BLOCK_FIELDS})
+    b = batch or A.Batch([192], [384], [6], [32])
+    A.ardit_stack_fwd_mx(FAKE, d, b, x, [kv or _mx()], mod, [ctx], [ctx], [w], out, FAKE, nbytes)
+
+
+def _chunk(batch=None, kv=None, steps=(2,), ts=((900.0, 400.0),), x0=1 << 30, nbytes=1 << 28, noise=FAKE):
+    d = _dims()
+    w = A.block_weights({k: FAKE for k in A._BLOCK_FIELDS})
+    tw = A.time_weights({k: FAKE for k in A._TIME_FIELDS})
+    b = batch or A.Batch([192], [384], [6], [32])
+    A.ardit_chunk_generate_mx(FAKE, d, b, list(steps), ts, FAKE, noise, [kv or _mx()], tw, [FAKE], [FAKE], [w], x0,
+                              FAKE, nbytes)
+
+
+@pytest.mark.parametrize("call", [_stack, _chunk])
+def test_model_path_refusals(call):
+    assert _status(lambda: call(kv=_mx(fmt=7))) == -1
+    assert _status(lambda: call(kv=_mx(vs=0))) == -1
+    assert _status(lambda: call(kv=_mx(max_frames=8))) == -3
+    assert _status(lambda: call(batch=A.Batch([192], [384], [6], [32], sparsity=[0.5]))) == -5
+    assert _status(lambda: call(batch=A.Batch([100], [384], [6], [32]))) == -2
+    assert _status(lambda: call(batch=A.Batch([192], [100], [6], [32]))) == -2
+    assert _status(lambda: call(batch=A.Batch([192], [384], [6], [0]))) == -2
+    assert _status(lambda: call(nbytes=1024)) == -4
+
+
+def test_stack_and_chunk_refusals():
+    assert _status(lambda: _stack(x=FAKE, out=FAKE)) == -1
+    assert _status(lambda: _stack(mod=0)) == -1
+    assert _status(lambda: _stack(ctx=0)) == -1
+    wide = _dims(dim=512, head_dim=128)
+    assert _status(lambda: _stack(dims=wide, batch=A.Batch([192], [384], [6], [32], quant=[1]))) == -5
+    assert _status(lambda: _chunk(steps=(17,), ts=((0.0,) * 17,))) == -1
+    assert _status(lambda: _chunk(ts=((900.0, 1400.0),))) == -1
+    assert _status(lambda: _chunk(noise=0)) == -1
+    assert _status(lambda: _chunk(x0=FAKE)) == -1            # over x_init
