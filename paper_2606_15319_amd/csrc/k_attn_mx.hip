@@ -205,11 +205,12 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   const bool solo = L >= a.solo_item;
   const int item = solo ? (L - a.solo_item) * SM_WAVES + wave : L;
   if (solo && item >= a.solo_waves) return;
-  int si = solo ? a.solo_span : 0;
-  const int last_span = solo ? a.n_spans : a.solo_span;
-  for (int i = si + 1; i < last_span; ++i)
-    if (item >= a.s[i].item_begin) si = i;
-  const MxSpan S = a.s[si];
+  // the last span that begins at or before the item: a lane looks at one of the others
+  // (one after the other they cost a scalar load and a wait each)
+  const int span0 = solo ? a.solo_span : 0, spans = (solo ? a.n_spans : a.solo_span) - span0;
+  const int si = span0 + __builtin_popcountll(__ballot(lane + 1 < spans &&
+                                                       item >= a.s[min(span0 + lane + 1, kMaxStreams)].item_begin));
+  const MxSpan S = a.s[__builtin_amdgcn_readfirstlane(si)];
   const int it = item - S.item_begin;
   const int hp = it / S.n_qtiles, qt = it - hp * S.n_qtiles;
   const int h = hp / S.pieces, piece = hp - h * S.pieces;
@@ -331,14 +332,19 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-    const float m_new = fmaxf(m_run, pair_max(mx) * c);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    m_run = m_new;
-    l_run *= alpha;
+    mx = pair_max(mx) * c;
+    // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
+    // 2^8), so that o is seldom rescaled
+    if (__any(mx > m_run + 8.0f)) {
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
     bf16x8 pf[4];
     const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
@@ -347,8 +353,8 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 8 * (k & 1) + 2 * j;
-        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_new)),
-                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_new)));
+        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run)),
+                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_run)));
         l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
       }
       pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
@@ -447,37 +453,60 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
 }
 
 // Joins the partial results of a row: those of its stream's cuts and, when the batch
-// shares a prefix, of the prefix's.
+// shares a prefix, of the prefix's.  HD / 4 lanes hold a row; a.groups such groups, at
+// least a wave, take the cuts in turn and meet in LDS (one group for all of them took
+// 16 us for 27 cuts, one trip to memory after the other; 4.8 us so).
 template <int HD>
 __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) {
-  constexpr int TPR = HD / 4, RPB = 256 / TPR;
-  const int i = static_cast<int>(blockIdx.x) * RPB + static_cast<int>(threadIdx.x) / TPR;   // head-major rows
-  const int c4 = threadIdx.x % TPR;
-  const int h = i / a.rows, r = i - h * a.rows;
-  if (h >= a.p.H) return;
-  int si = -1;   // (streams in any order; each holds its rows once)
-  for (int j = a.shared; j < a.n_spans; ++j)
-    if (r >= a.s[j].q_off && r < a.s[j].q_off + a.s[j].q_len) si = j;
-  if (si < 0) return;            // a row of the other kernel's
-  const MxSpan& S = a.s[si];
-  if (S.part_begin < 0) return;   // written whole
+  constexpr int TPR = HD / 4, NG = 256 / TPR;
+  __shared__ float4 part_o[NG][TPR];
+  __shared__ float2 part_ml[NG];
+  const int grp = static_cast<int>(threadIdx.x) / TPR, c4 = threadIdx.x % TPR, lane = threadIdx.x & 63;
+  const int sub = grp & (a.groups - 1);
+  const int i = (static_cast<int>(blockIdx.x) * NG + grp) / a.groups;   // head-major rows, one to a wave
+  const int h = __builtin_amdgcn_readfirstlane(i / a.rows), r = __builtin_amdgcn_readfirstlane(i - h * a.rows);
+  // the stream's span (in any order; each holds its rows once)
+  const MxSpan& mine = a.s[min(a.shared + lane, kMaxStreams)];
+  const uint64_t hit = __ballot(a.shared + lane < a.n_spans && r >= mine.q_off && r - mine.q_off < mine.q_len);
+  const int si = a.shared + (hit ? __builtin_ctzll(hit) : 0);
+  const MxSpan S = a.s[__builtin_amdgcn_readfirstlane(si)];
+  // (a row of the other kernel's, or written whole: nothing to join)
+  const bool join = h < a.p.H && hit != 0 && S.part_begin >= 0;
   const MxSpan& P = a.s[0];
-  const int own = S.pieces, all = own + (a.shared ? P.pieces : 0);
-  auto slot = [&](int j) {
-    return j < own ? S.part_begin + (static_cast<size_t>(h) * own + j) * S.q_len + (r - S.q_off)
-                   : P.part_begin + (static_cast<size_t>(h) * P.pieces + j - own) * P.q_len + r;
-  };
-  float M = kNoMax;
-#pragma unroll 8
-  for (int j = 0; j < all; ++j) M = fmaxf(M, a.part_ml[slot(j)].x);
-  float l = 0.f;
+  const int own = S.pieces, all = join ? own + (a.shared ? P.pieces : 0) : 0;
+  float M = kNoMax, l = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int j = 0; j < all; ++j) {
-    const size_t at = slot(j);
+#pragma unroll 4
+  for (int j = sub; j < all; j += a.groups) {
+    const size_t at = j < own ? S.part_begin + (static_cast<size_t>(h) * own + j) * S.q_len + (r - S.q_off)
+                              : P.part_begin + (static_cast<size_t>(h) * P.pieces + j - own) * P.q_len + r;
     const float2 ml = a.part_ml[at];
-    const float wgt = __builtin_amdgcn_exp2f(ml.x - M);
     const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * HD + 4 * c4);
+    const float m_new = fmaxf(M, ml.x);
+    const float keep = __builtin_amdgcn_exp2f(M - m_new), wgt = __builtin_amdgcn_exp2f(ml.x - m_new);
+    M = m_new;
+    l = l * keep + wgt * ml.y;
+    acc.x = acc.x * keep + wgt * x.x;
+    acc.y = acc.y * keep + wgt * x.y;
+    acc.z = acc.z * keep + wgt * x.z;
+    acc.w = acc.w * keep + wgt * x.w;
+  }
+  part_o[grp][c4] = acc;
+  if (c4 == 0) part_ml[grp] = make_float2(M, l);
+  __syncthreads();
+  if (sub != 0 || !join) return;
+  const float own_m = M;
+  for (int g = 1; g < a.groups; ++g) M = fmaxf(M, part_ml[grp + g].x);
+  const float first = __builtin_amdgcn_exp2f(own_m - M);
+  l *= first;
+  acc.x *= first;
+  acc.y *= first;
+  acc.z *= first;
+  acc.w *= first;
+  for (int g = 1; g < a.groups; ++g) {
+    const float2 ml = part_ml[grp + g];
+    const float wgt = __builtin_amdgcn_exp2f(ml.x - M);
+    const float4 x = part_o[grp + g][c4];
     l += wgt * ml.y;
     acc.x += wgt * x.x;
     acc.y += wgt * x.y;
@@ -947,8 +976,8 @@ template <int HD, int BITS>
 hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
   hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
   if (a.join) {
-    constexpr int RPB = 256 / (HD / 4);
-    hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + RPB - 1) / RPB), dim3(256), 0, st, a);
+    const int per = 256 / (HD / 4) / a.groups;   // rows of a workgroup
+    hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + per - 1) / per), dim3(256), 0, st, a);
   }
   return hipGetLastError();
 }
@@ -1044,6 +1073,12 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
       a.join = 1;
     }
   }
+  // groups of the join's lanes: four cuts each, of the row with most
+  int cuts = 1;
+  for (int i = a.shared; i < a.n_spans; ++i) cuts = std::max(cuts, a.s[i].pieces + (a.shared ? a.s[0].pieces : 0));
+  const int lanes = a.p.hd / 4;
+  a.groups = kWave / lanes;
+  while (a.groups < 256 / lanes && 4 * a.groups < cuts) a.groups *= 2;
   a.solo_item = static_cast<int32_t>(items);
   a.solo_waves = static_cast<int32_t>(solo);
   a.total_items = static_cast<int32_t>(items + (solo + SM_WAVES - 1) / SM_WAVES);

@@ -278,7 +278,7 @@ struct MxSmallArgs {
   int32_t ld;
   float scale_log2;      // log2(e) / sqrt(d)
   int32_t n_spans, shared;   // shared: span 0 is the common prefix, of all rows
-  int32_t join;          // some span leaves partial results
+  int32_t join, groups;  // some span leaves partial results; groups of lanes that join a row's
   int32_t total_items, per_xcd;   // workgroups
   int32_t solo_span;     // spans from here on: a cut is a wave's, not a workgroup's
   int32_t solo_item, solo_waves;  // first workgroup of theirs, and their waves in all
