@@ -983,7 +983,7 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
 }
 
 constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
-constexpr int kSmallStart = 4;     // a workgroup's start and end, in tiles of a wave
+constexpr int kSmallStart = 3;     // a workgroup's start and end, in tiles of a wave
 // Most rows and tiles of a solo span.  32 continuations of one history, half of them with
 // a frame of their own: 89 us with a workgroup for each, 77 up to 16 tiles, 54 up to 32 or
 // 64; with 12 and 24 rows of partial results a wave it loses (six spans of 10 heads of
@@ -1118,7 +1118,7 @@ static int64_t plan_few(MxSmallArgs& a, const RowStreams& rs, int rows_most, int
     s.tile1 = static_cast<int32_t>(mx_tiles(s.kv_len, p.T, p.nt));
   }
   const int64_t end = plan_small(a, max_rows);
-  return p.hd == 128 ? 730 + 105 * end : 690 + 67 * end;
+  return p.hd == 128 ? 800 + 105 * end : 710 + 68 * end;
 }
 
 // The estimated end of whole-chunk items of the streams with more rows, likewise.
@@ -1134,17 +1134,17 @@ static int64_t estimate_many(const MxPages& p, const RowStreams& rs, int rows_ov
   }
   // (a round that the items leave idle is split; whole items go in rounds)
   const int64_t tiles = items < 3 * kSmallRound / 4 ? work / kSmallRound : std::max(most, work / kSmallRound);
-  return p.hd == 128 ? 3260 + 122 * tiles : 2510 + 89 * tiles;
+  return p.hd == 128 ? 3260 + 123 * tiles : 2620 + 89 * tiles;
 }
 
 // Which kernel takes a stream goes by estimates fitted to 360 calls (1 to 8 streams of
 // 64 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
 // both formats), each timed on both: a tile of a wave, eight at a time on a CU, takes
-// 2.1 us at d = 128 and 1.35 at d = 64 after 7 us; a tile of 256 rows 1.22 and 0.89
-// after 33 and 25 (a split schedule and its merge).  The choice loses 0.6% to the better
-// one on average.  us of few rows' kernel and of whole-chunk items, 12 heads of 128 over
-// 32760 tokens: 64 rows 39 / 62, 192 66 / 76, 256 88 / 79, 768 321 / 159; four streams of
-// 100 181 / 156, eight of 64 197 / 267.
+// 2.1 us at d = 128 and 1.36 at d = 64 after 8 and 7 us; a tile of 256 rows 1.23 and 0.89
+// after 33 and 26 (a split schedule and its merge).  The choice loses 0.6% to the better
+// one on average, 15% at most.  us of the few rows' kernel and of whole-chunk items, 12
+// heads of 128 over 32760 tokens: 64 rows 33 / 62, 192 63 / 76, 256 83 / 81, 768 304 / 165;
+// four streams of 100 171 / 155, eight of 64 196 / 269.
 hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
                                const RowStreams& rs, int shared, float* part) {
   MxSmallArgs a;
