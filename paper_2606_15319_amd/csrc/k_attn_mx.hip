@@ -326,6 +326,20 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 16 * b + i < left ? s[b][i] : -INFINITY;
+      // Values past the end are zero: whatever the page holds there would meet a zero
+      // weight.  Codes are cut with one mask a word for all dims of a lane (six ragged
+      // streams over pages of 72 keys 66 us with their bf16 values cut, 53 so).  A block
+      // without keys may hold any scale.
+      constexpr int PER = 32 / BITS;   // codes of a word
+#pragma unroll
+      for (int w = 0; w < BITS; ++w) {
+        const int n_in = left - PER * w;
+        const uint32_t mask = n_in >= PER ? ~0u : (n_in <= 0 ? 0u : (1u << (BITS * n_in)) - 1u);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) vw[db][w >> 2][w & 3] &= mask;
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vsb[db] = left > 0 ? vsb[db] : 127u;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -367,8 +381,6 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
         u32x4 x;
         if constexpr (BITS == 8) x = mx_decode8<8>(vw[db][k >> 1][2 * (k & 1)], vw[db][k >> 1][2 * (k & 1) + 1], sc);
         else x = mx_decode8<4>(vw[db][0][k], 0u, sc);
-        // values past the end are zero: whatever the page holds there would meet a zero weight
-        if (keys < 64) x = keep_first(x, keys - 32 * hh - 8 * k);
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pf[k], o[db], 0, 0, 0);
       }
     }
