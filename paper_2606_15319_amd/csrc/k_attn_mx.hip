@@ -150,6 +150,18 @@ __device__ __forceinline__ void scores(const i32x8 (&k)[2][HD / 64], const uint3
   }
 }
 
+// Weights p[i0 .. i0 + 8) as one operand of the value product; sum: their sum as rounded.
+__device__ __forceinline__ bf16x8 pack_weights(const f32x16& p, int i0, float& sum) {
+  const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    w[j] = pack_bf16x2(p[i0 + 2 * j], p[i0 + 2 * j + 1]);
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, sum, false);
+  }
+  return __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+}
+
 // 16-byte chunk c of an LDS row of ROWB bytes sits at chunk c ^ swz(r): 16 rows then
 // cover every bank for a fixed c.
 template <int ROWB>
@@ -360,18 +372,12 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
     bf16x8 pf[4];
-    const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      uint32_t w[4];
+      f32x16 w;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 8 * (k & 1) + 2 * j;
-        w[j] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run)),
-                           __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i + 1], c, -m_run)));
-        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
-      }
-      pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+      for (int i = 8 * (k & 1); i < 8 * (k & 1) + 8; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run));
+      pf[k] = pack_weights(w, 8 * (k & 1), l_run);
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -671,7 +677,16 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
 #pragma unroll
   for (int k = 0; k < 4; ++k) v_at[k] = n32 * 128 + (((4 * hh + k) ^ swz<128>(n32)) << 4);
 
-  f32x16 o[DB], s[2], p_[2];   // p_: weights of the last VALU phase
+  // At d = 128 weights are formed against the running maximum as it is and summed at once:
+  // a row whose weights sum to more than 2^14 (or to no number) raises the maximum and forms
+  // them again, and a tile's maximum is seldom needed (1497 -> 1459 us over 37440 tokens, 20
+  // heads, 4 bits; 8 bits 1540 -> 1519).  At d = 64 the products are half as long and the
+  // maxima are taken beside them, the weights packed beside the next tile's scores (502 us
+  // for 548, 4680 queries over 14040 tokens, 20 heads).
+  constexpr bool SUMS = HD == 128;
+  f32x16 o[DB], s[2];
+  f32x16 p_[2];                // !SUMS: weights of the last VALU phase
+  bf16x8 pf[4];                // weights as the products take them
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -749,18 +764,9 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int db = 0; db < DB; ++db) vf[k][db] = *reinterpret_cast<const bf16x8*>(tv + v_at[k] + 4096 * db);
-      const bf16x2 one2 = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
-      bf16x8 pf[4];
+      if constexpr (!SUMS) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 8 * (k & 1) + 2 * j;
-          w[j] = pack_bf16x2(p_[k >> 1][i], p_[k >> 1][i + 1]);
-          l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[j]), one2, l_run, false);
-        }
-        pf[k] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+        for (int k = 0; k < 4; ++k) pf[k] = pack_weights(p_[k >> 1], 8 * (k & 1), l_run);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -770,13 +776,23 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     }
     if constexpr (QK) {
       convert(t, no, 64);
-      tile_max();
+      if constexpr (!SUMS) tile_max();
     }
-    asm volatile("" : "+v"(top), "+v"(l_run));
+    if constexpr (!SUMS) asm volatile("" : "+v"(top), "+v"(l_run));
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  auto raise_max = [&]() __attribute__((always_inline)) {   // to the tile's, where that is more
+    const float m_new = fmaxf(m_run, top * c);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+  };
   // VALU phase: the weights of the scores
   auto softmax = [&](int keys) __attribute__((always_inline)) {
     if (keys < 64) {
@@ -785,26 +801,39 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 16 * b + i < left ? s[b][i] : -INFINITY;
-      tile_max();
+      if constexpr (!SUMS) tile_max();
     }
-    const float mx = top * c;
-    // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
-    // 2^8), so that o is seldom rescaled
-    if (__any(mx > m_run + 8.0f)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-      m_run = m_new;
-      l_run *= alpha;
+    if constexpr (SUMS) {
+      float s0 = 0.f, s1 = 0.f;
+      auto weigh = [&]() __attribute__((always_inline)) {
+        s0 = s1 = 0.f;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+        for (int k = 0; k < 4; ++k) {
+          f32x16 p;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+          for (int i = 8 * (k & 1); i < 8 * (k & 1) + 8; ++i)
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run));
+          pf[k] = pack_weights(p, 8 * (k & 1), k & 1 ? s1 : s0);
+        }
+      };
+      weigh();
+      if (__any(!(s0 + s1 <= 16384.f))) {
+        tile_max();
+        raise_max();
+        weigh();
+      }
+      l_run += s0 + s1;
+      asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]), "+v"(l_run));
+    } else {
+      // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
+      // 2^8), so that o is seldom rescaled
+      if (__any(top * c > m_run + 8.0f)) raise_max();
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p_[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m_run));
+      asm volatile("" : "+v"(p_[0]), "+v"(p_[1]));
     }
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p_[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m_run));
-    asm volatile("" : "+v"(p_[0]), "+v"(p_[1]));
   };
 
   // ---- prologue: the positions ahead of the group's first VALU phase
