@@ -59,16 +59,20 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t m) {   // over 4 neighbour
 // Queries and keys of RPW rows a wave.  Keys are normed and rotated in fp64 up to their
 // rounding to codes: a code's step is up to an eighth of its value, and with fp32's last
 // bits in doubt a few of seven million keys lie close enough to a border to take the other
-// code (2 us of 29 at 4680 rows of 1536, 7 of 187 at 9360 of 5120).  Rows of more than 1024
-// dims go one to a wave: fewer registers, more rows under way (29 us for 32).
-// A lane holds chunks lane + 64 i of 8 dims of
-// a row, so a block of 32 dims is four neighbouring lanes and a head 16 or 8 of them.
-template <int MAXC, int RPW, int BITS>
+// code.  Rows of more than 1024 dims go one to a wave and wider ones to two or four waves,
+// so that a lane holds three or four pieces: fewer registers, more rows under way (with
+// their read-back, 4680 rows of 1536 29 us for 32 with two rows a wave, 9360 of 5120 169
+// for 186 with a wave each).  A lane holds chunks lane + 64 (part + WPR i) of 8 dims of a
+// row, so a block of 32 dims is four neighbouring lanes and a head 16 or 8 of them.
+template <int MAXC, int RPW, int WPR, int BITS>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, float* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = (group * 4 + wave) * RPW;
-  const int nchunk = a.D >> 3, hd = a.p.hd;
-  double* lcs = reinterpret_cast<double*>(lds) + wave * RPW * 128;   // cos and sin of each row's pairs
+  const int set = wave / WPR, part = wave % WPR;   // WPR waves hold the rows of a set
+  const int row0 = (group * (4 / WPR) + set) * RPW;
+  const int nchunk = a.D >> 3, hd = a.p.hd, lane0 = lane + 64 * part;
+  double* lcs = reinterpret_cast<double*>(lds) + set * RPW * 128;   // cos and sin of each row's pairs
+  __shared__ double part_sk[4][RPW];
+  __shared__ float part_sq[4][RPW];
 
   uint4 qraw[RPW][MAXC], kraw[RPW][MAXC];
 #pragma unroll
@@ -76,7 +80,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
     const uint4* qr = reinterpret_cast<const uint4*>(a.qkv + static_cast<size_t>(min(row0 + r, a.N - 1)) * 3 * a.D);
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
-      const int c = lane + 64 * i;
+      const int c = lane0 + 64 * WPR * i;
       if (c < nchunk) {
         qraw[r][i] = qr[c];
         kraw[r][i] = qr[nchunk + c];
@@ -85,6 +89,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
   }
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
+    if (WPR > 1 && r % WPR != part) continue;
     const int row = min(row0 + r, a.N - 1);
     const RowStream s = a.rs.s[stream_of(a.rs, row)];
     const int t = row - s.row_begin;
@@ -103,17 +108,13 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
     lcs[r * 128 + lane] = cs;
     lcs[r * 128 + 64 + lane] = sn;
   }
-  // (a wave's own rows: no barrier, its LDS operations stay in order)
-  __builtin_amdgcn_wave_barrier();
-
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {
-    const int row = row0 + r;
     float sq = 0.f;
     double sk = 0.0;
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
-      if (lane + 64 * i < nchunk) {
+      if (lane0 + 64 * WPR * i < nchunk) {
         float x[8], y[8];
         unpack8(qraw[r][i], x);
         unpack8(kraw[r][i], y);
@@ -126,6 +127,25 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
     }
     sq = wave_sum(sq);
     sk = wave_sum64(sk);
+    if (lane == 0) {
+      part_sq[wave][r] = sq;
+      part_sk[wave][r] = sk;
+    }
+  }
+  // (a wave's own rows need no barrier: its LDS operations stay in order)
+  if constexpr (WPR > 1) __syncthreads();
+  else __builtin_amdgcn_wave_barrier();
+
+#pragma unroll
+  for (int r = 0; r < RPW; ++r) {
+    const int row = row0 + r;
+    float sq = 0.f;
+    double sk = 0.0;
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) {
+      sq += part_sq[set * WPR + w][r];
+      sk += part_sk[set * WPR + w][r];
+    }
     if (row >= a.N) continue;
     const float rq = 1.0f / sqrtf(sq / static_cast<float>(a.D) + a.eps);
     const double rk = 1.0 / sqrt(sk / static_cast<double>(a.D) + static_cast<double>(a.eps));
@@ -139,7 +159,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
     uint4* qo = reinterpret_cast<uint4*>(a.q_out + static_cast<size_t>(row) * a.D);
 #pragma unroll
     for (int i = 0; i < MAXC; ++i) {
-      const int c = lane + 64 * i;
+      const int c = lane0 + 64 * WPR * i;
       if (c < nchunk) {
         const int e0 = (8 * c) & (hd - 1);
         const int h = (8 * c) / hd;
@@ -255,8 +275,8 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, int w, uint32
 }
 
 // Rows and value tiles in one launch, so the two run side by side.
-template <int MAXC, int RPW, int BITS>
-__global__ __launch_bounds__(256, MAXC == 6 || MAXC == 10 ? 4 : 1) void kv_append_mx_kernel(const AppendArgs a) {
+template <int MAXC, int RPW, int WPR, int BITS>
+__global__ __launch_bounds__(256) void kv_append_mx_kernel(const AppendArgs a) {
   __shared__ __attribute__((aligned(16))) uint32_t lds[64 * 64];
   const int b = blockIdx.x;
   if (b < a.qk_groups) {
@@ -265,7 +285,7 @@ __global__ __launch_bounds__(256, MAXC == 6 || MAXC == 10 ? 4 : 1) void kv_appen
     const int per = (a.qk_groups + kNumXcd - 1) / kNumXcd;
     int g = b;
     if (a.qk_groups % kNumXcd == 0) g = (b % kNumXcd) * per + b / kNumXcd;
-    append_rows<MAXC, RPW, BITS>(a, g, reinterpret_cast<float*>(lds));
+    append_rows<MAXC, RPW, WPR, BITS>(a, g, reinterpret_cast<float*>(lds));
   } else {
     append_values<BITS>(a, b - a.qk_groups, lds);
   }
@@ -376,22 +396,25 @@ hipError_t launch_kv_append_mx(hipStream_t st, const bf16_t* qkv, int N, const R
     for (int k = 0; k < seg / 2; ++k)
       a.inv_freq[pair++] = pow(static_cast<double>(g.theta), -2.0 * k / seg) / 6.283185307179586;
   a.rs = rs;
+  // chunks of a lane, rows of a wave and waves of a row by the row's width
   const int chunks = (g.D / 8 + 63) / 64;
-  const int rpw = chunks <= 2 ? 2 : 1;
-  a.qk_groups = (N + 4 * rpw - 1) / (4 * rpw);
-  const dim3 grid(a.qk_groups + a.v_tiles * g.H);
-#define ARDIT_APPEND_CASE(C, R)                                                                   \
-  do {                                                                                            \
-    if (pages.bits == 8) hipLaunchKernelGGL((kv_append_mx_kernel<C, R, 8>), grid, dim3(256), 0, st, a); \
-    else hipLaunchKernelGGL((kv_append_mx_kernel<C, R, 4>), grid, dim3(256), 0, st, a);           \
+  int rows = 0;   // of a workgroup
+#define ARDIT_APPEND_CASE(C, R, W)                                                                   \
+  do {                                                                                               \
+    rows = 4 / W * R;                                                                                \
+    a.qk_groups = (N + rows - 1) / rows;                                                             \
+    const dim3 grid(a.qk_groups + a.v_tiles * g.H);                                                  \
+    if (pages.bits == 8) hipLaunchKernelGGL((kv_append_mx_kernel<C, R, W, 8>), grid, dim3(256), 0, st, a); \
+    else hipLaunchKernelGGL((kv_append_mx_kernel<C, R, W, 4>), grid, dim3(256), 0, st, a);           \
   } while (0)
-  if (chunks <= 1) ARDIT_APPEND_CASE(1, 2);
-  else if (chunks <= 2) ARDIT_APPEND_CASE(2, 2);
-  else if (chunks <= 3) ARDIT_APPEND_CASE(3, 1);
-  else if (chunks <= 4) ARDIT_APPEND_CASE(4, 1);
-  else if (chunks <= 6) ARDIT_APPEND_CASE(6, 1);
-  else if (chunks <= 10) ARDIT_APPEND_CASE(10, 1);
-  else ARDIT_APPEND_CASE(16, 1);
+  if (chunks <= 1) ARDIT_APPEND_CASE(1, 2, 1);
+  else if (chunks <= 2) ARDIT_APPEND_CASE(2, 2, 1);
+  else if (chunks <= 3) ARDIT_APPEND_CASE(3, 1, 1);
+  else if (chunks <= 4) ARDIT_APPEND_CASE(4, 1, 1);
+  else if (chunks <= 6) ARDIT_APPEND_CASE(3, 1, 2);
+  else if (chunks <= 8) ARDIT_APPEND_CASE(4, 1, 2);
+  else if (chunks <= 12) ARDIT_APPEND_CASE(3, 1, 4);
+  else ARDIT_APPEND_CASE(4, 1, 4);
 #undef ARDIT_APPEND_CASE
   return hipGetLastError();
 }

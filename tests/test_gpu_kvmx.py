@@ -126,7 +126,10 @@ APPENDS = [   # H, d, (lat_h, lat_w), frames, cached frames per stream, first po
     (2, 128, (6, 12), 1, [0, 5, 1], [0, 7, 100000]),       # T = 72: a tile of 8 keys behind a whole one
     (10, 64, (4, 8), 2, [3, 0], [3, 9]),                   # T = 32: half a tile
     (1, 128, (7, 8), 3, [1], [1]),                         # T = 56, width 128
-    (33, 128, (8, 8), 1, [0], [2]),                        # rows of 4224: nine chunks a lane
+    (13, 128, (8, 8), 1, [1], [2]),                        # rows of 1664: one to a wave
+    (20, 128, (6, 12), 1, [0], [3]),                       # 2560: one to two waves
+    (32, 128, (8, 8), 1, [0], [0]),                        # 4096: the widest of those
+    (33, 128, (8, 8), 1, [0], [2]),                        # 4224: one to four waves
     (64, 128, (8, 8), 1, [1], [4]),                        # the widest rows
     (12, 128, (30, 52), 1, [1], [11]),
 ]
