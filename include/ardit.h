@@ -170,7 +170,8 @@ typedef enum {
  * (E4M3) or at most 6 (E2M1), so that no code saturates; its byte is e + 127, and
  * 255 marks a block that held an infinity or NaN, every value of which reads back
  * as NaN.  Codes are rounded to nearest, ties to even.  Every value is exact in
- * bf16.
+ * bf16.  (At bf16's end: in E2M1 e is at most 125 and values past 6 2^125 = 2.6e38
+ * become that; E4M3 rounds those of 248 2^120 = 3.3e38 and more to infinity.)
  * A page holds tiles of 64 keys: with T64 = T rounded up to 64 and n = T64 / 64,
  *   k_codes  [n_pages][H][T64][d] codes      k_scales [n_pages][H][T64][d / 32]
  *   v_codes  [n_pages][H][n][d][64] codes    v_scales [n_pages][H][n][2][d]

@@ -6,8 +6,8 @@ each attention product's summed axis, with a power of two 2^e per block:
   - values: 32 consecutive keys of one page, per dim (a page's last block may
     hold fewer);
   - e is the smallest exponent, at least -117, with max|x| / 2^e below 256
-    (E4M3) or at most 6 (E2M1); an all-zero block takes -117; a block with an
-    infinity or NaN reads back as NaN;
+    (E4M3) or at most 6 (E2M1), there at most 125 (6 2^126 is past bf16); an
+    all-zero block takes -117; a block with an infinity or NaN reads back as NaN;
   - codes are the nearest values of the format, ties to the even code.
 
 A page of T tokens lies in tiles of 64 keys (T64 = T rounded up): k_codes
@@ -41,10 +41,10 @@ def grid(bits: int) -> np.ndarray:
 
 
 def exponent(amax, bits: int):
-    """Smallest e >= -117 with amax / 2^e < 256 (8 bits) or <= 6 (4 bits)."""
+    """Smallest e >= -117 with amax / 2^e < 256 (8 bits) or <= 6 (4 bits, e <= 125)."""
     amax = np.asarray(amax, np.float64)
     m, ex = np.frexp(np.where(amax > 0, amax, 1.0))       # amax = m 2^ex, m in [0.5, 1)
-    e = ex - 8 if bits == 8 else np.where(m <= 0.75, ex - 3, ex - 2)
+    e = ex - 8 if bits == 8 else np.minimum(np.where(m <= 0.75, ex - 3, ex - 2), 125)
     return np.where(amax > 0, np.maximum(e, MIN_EXP), MIN_EXP).astype(np.int64)
 
 

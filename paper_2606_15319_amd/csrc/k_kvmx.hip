@@ -132,9 +132,10 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
       part_sk[wave][r] = sk;
     }
   }
-  // (a wave's own rows need no barrier: its LDS operations stay in order)
+  // (a wave's own rows need no barrier: its LDS operations stay in order, the fence
+  // keeps the compiler from moving them)
   if constexpr (WPR > 1) __syncthreads();
-  else __builtin_amdgcn_wave_barrier();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 
 #pragma unroll
   for (int r = 0; r < RPW; ++r) {

@@ -97,13 +97,14 @@ def _attend(A, pool, q_lens, caches, q, shared=0, stream=None, ws=None, o=None):
     return o
 
 
-def _check_attention(got, q, k, v, rows=None):
+def _check_attention(got, q, k, v, independent=True):
     """got [R, H, d] against float64.  Rounding the weights to bf16 moves the numerator by
     at most 2^-8 sum p |v|, the denominator (a sum of the rounded weights) by 2^-8 of itself;
     the store rounds by 2^-8; 2^-10 more of the weights covers the scores (queries split
     into two E4M3 parts, 2^-21 of a block's largest element per product, and fp32 sums)
     and exp2.  Over many keys the errors cancel: a weight's is uniform within its half
-    step, at most 2^-8 / sqrt(3) of it, independent of the others."""
+    step, at most 2^-8 / sqrt(3) of it, independent of the others (not those of a key that
+    comes again: then only the first bound holds)."""
     d = q.shape[-1]
     s = np.einsum("rhd,khd->hrk", q, k) / math.sqrt(d)
     p = np.exp(s - s.max(-1, keepdims=True))
@@ -113,6 +114,8 @@ def _check_attention(got, q, k, v, rows=None):
     err = np.abs(got - ref)
     tiny = 2.0 ** -120
     assert np.all(err <= (2.0 ** -7 + 2.0 ** -10) * spread + 2.0 ** -8 * np.abs(ref) + tiny)
+    if not independent:
+        return
     p2 = p * p
     var = np.einsum("hrk,khd->rhd", p2, v * v) + p2.sum(-1).T[:, :, None] * ref * ref
     sd = 2.0 ** -8 / math.sqrt(3) * np.sqrt(var + ref * ref) + 2.0 ** -10 * np.sqrt(var) + tiny
@@ -571,3 +574,97 @@ def test_a_chunk_written_and_attended(A):
                       O.chunk_positions(frames, *lat, chunk * frames), 10000.0)
         k = np.concatenate(held_k[-frames:])
         assert np.all(np.abs(k - kr) <= np.abs(M.rounded(kr, 8) - kr) + 4e-5)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_values_at_the_end_of_bf16(A, bits):
+    """The largest numbers: 4 bits stop at 6 2^125, 8 bits round 248 2^120 and more to infinity."""
+    import torch
+    H, d, T = 2, 64, 64
+    D = H * d
+    pool = Pool(A, H, d, (8, 8), 1, bits, [T], fill=0)
+    pool.upload()
+    rng = make_rng(131)
+    qkv = normal_bf16(rng, (T, 3 * D)).astype(np.float32)
+    v = qkv[:, 2 * D:]
+    end = np.float32(255 * 2.0 ** 120)           # the largest bf16 number
+    v[:, 0] = end
+    v[::2, 1], v[1::2, 1] = -end, np.float32(2.0 ** 126)
+    v[:, 2] = np.float32(247 * 2.0 ** 120)
+    v[:, 3] = np.float32(1.5 * 2.0 ** 127)       # 6 2^125 itself
+    v[:, 4] = -np.float32(2.0 ** 127)
+    dev = dev_bf16(qkv)
+    assert np.array_equal(host_f32(dev)[:, 2 * D:2 * D + 5], v[:, :5])
+    one = dev_bf16(np.ones(D, np.float32))
+    q = torch.empty((T, D), dtype=torch.bfloat16, device="cuda")
+    A.ardit_kv_append_mx(None, pool.dims, A.Batch([T], [0], [0]), dev, one, one, pool.kv(), q)
+    k16 = torch.zeros((1, H, T, d), dtype=torch.bfloat16, device="cuda")
+    v16 = torch.zeros((1, H, d, T), dtype=torch.bfloat16, device="cuda")
+    A.ardit_kv_read_mx(None, pool.dims, A.Batch([T], [0]), pool.kv(),
+                       A.kv_paged(k16, v16, dev_i32(np.zeros((1, 1), np.int32)), 1, 1))
+    _sync()
+    want = M.rounded(host_f32(dev)[:, 2 * D:].astype(np.float64).reshape(T, H, d), bits, 0)
+    if bits == 8:
+        assert (want[:, 0, 0] == 2.0 ** 128).all() and np.abs(want[:, 0, 2:5]).max() < 2.0 ** 128
+        want = np.where(np.abs(want) == 2.0 ** 128, np.copysign(np.inf, want), want)
+    else:
+        assert (want[:, 0, 0] == 6 * 2.0 ** 125).all()
+    assert np.array_equal(host_f32(v16)[0].transpose(2, 0, 1), want)
+    pool.download()
+    assert np.array_equal(host_f32(k16)[0].transpose(1, 0, 2), pool.host.unpack(pool.ids[0][0])[0])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_queries_that_are_not_finite_stay_rows_of_their_own(A, d, rows):
+    """A NaN or an infinity in a query makes NaN of its row and head, the others are as without it."""
+    H, lat, T = 2, (8, 8), 64
+    pool = Pool(A, H, d, lat, 1, 8, [9 * T + rows], seed=15)
+    held = pool.fill([9 * T + rows], 141)
+    q = normal_bf16(make_rng(142), (rows, H, d)).astype(np.float32)
+    q[1, 0, 7] = np.nan
+    q[2, 1, 40] = -np.inf
+    o = _attend(A, pool, [rows], [9 * T], dev_bf16(q.reshape(rows, -1)))
+    _sync()
+    got = host_f32(o).astype(np.float64).reshape(rows, H, d)
+    assert np.isnan(got[1, 0]).all() and np.isnan(got[2, 1]).all()
+    k, v = held[0]
+    for h in range(H):
+        rest = np.array([r for r in range(rows) if r != 1 + h])
+        _check_attention(got[rest][:, h:h + 1], q[rest][:, h:h + 1].astype(np.float64), k[:, h:h + 1], v[:, h:h + 1])
+
+
+@pytest.mark.parametrize("rows", [[2, 37], [300, 5]])
+def test_one_page_many_times_and_rows_behind_the_last(A, rows):
+    """Table entries that name a page again; arrays longer than the batch; knobs that ask for nothing."""
+    import torch
+    H, d, lat, T = 2, 128, (6, 12), 72
+    cached = [12, 7]
+    lens = [T, T]
+    pool = Pool(A, H, d, lat, 1, 4, lens, seed=16)
+    held = pool.fill(lens, 151)
+    table = np.array([[pool.ids[0][0]] * 17, [pool.ids[1][0], pool.ids[0][0]] + [pool.ids[1][0]] * 15], np.int32)
+    pool.table, pool.span = dev_i32(table), 17
+    q = normal_bf16(make_rng(152), (sum(rows), H, d))
+    o = torch.full((sum(rows) + 9, H * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    batch = A.Batch(rows, [c * T for c in cached], sparsity=[0.0, 0.0], quant=[0, 0])
+    n = A.ardit_workspace_size(pool.dims, batch)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    A.ardit_attn_fwd_mx(None, pool.dims, batch, dev_bf16(q.reshape(-1, H * d)), pool.kv(), 0, o, ws, n)
+    _sync()
+    assert (host_bits(o)[sum(rows):] == host_bits(torch.full_like(o[:1], float("nan")))[0]).all()
+    got = host_f32(o).astype(np.float64)[:sum(rows)].reshape(-1, H, d)
+    at = 0
+    for b, m in enumerate(rows):
+        keys = [np.concatenate([held[int(p == pool.ids[1][0])][i] for p in table[b]])[:cached[b] * T + m] for i in range(2)]
+        _check_attention(got[at:at + m], q[at:at + m].astype(np.float64), *keys, independent=False)
+        at += m
+    # and read back: the same page to two pages of the other pool
+    k16 = torch.zeros((2, H, T, d), dtype=torch.bfloat16, device="cuda")
+    v16 = torch.zeros((2, H, d, T), dtype=torch.bfloat16, device="cuda")
+    t16 = dev_i32(np.array([[1, 0] + [-1] * 15, [-1] * 17], np.int32))
+    A.ardit_kv_read_mx(None, pool.dims, A.Batch([2 * T, 0], [0, 0]), pool.kv(), A.kv_paged(k16, v16, t16, 2, 17))
+    _sync()
+    for i in range(2):
+        assert np.array_equal(host_f32(k16)[i].transpose(1, 0, 2), held[0][0])
+        assert np.array_equal(host_f32(v16)[i].transpose(2, 0, 1), held[0][1])
