@@ -176,8 +176,9 @@ __device__ __forceinline__ int swz(int r) { return (r / (256 / ROWB)) & (ROWB / 
 // one row tile leave partial results (unnormalised o, running maximum, denominator)
 // that a second kernel joins.  Spans of few tiles are solo: a cut is one wave's, and
 // the eight waves of a workgroup are on their own.
-// What bounds it: the cache's bytes.  Eight tokens over 9 to 21 frames each in 8 bits
-// 113 us, 4.8 TB/s; with four waves and rings of 32 KB 117 (in 4 bits 66 for 86).
+// What bounds it: the cache's bytes.  Eight tokens over 9 to 21 frames each, 12 heads of
+// 128, in 8 bits 106 to 110 us with the join's 5, 5 TB/s (in 4 bits 58); as first built,
+// with four waves and rings of 32 KB 117 for 113 (in 4 bits 86 for 66).
 constexpr int SM_BQ = 32;
 constexpr int SM_WAVES = 8;
 
@@ -472,8 +473,9 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
 
 // Joins the partial results of a row: those of its stream's cuts and, when the batch
 // shares a prefix, of the prefix's.  HD / 4 lanes hold a row; a.groups such groups, at
-// least a wave, take the cuts in turn and meet in LDS (one group for all of them took
-// 16 us for 27 cuts, one trip to memory after the other; 4.8 us so).
+// least a wave, take the cuts in turn and meet in LDS: one token over 32760 keys, one head,
+// 14 us for 16 with the groups of a wave (27 cuts: one group of lanes took 16 us for the
+// join alone, one trip to memory after the other, a wave of them 5).
 template <int HD>
 __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) {
   constexpr int TPR = HD / 4, NG = 256 / TPR;
@@ -1026,9 +1028,9 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
 constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
 constexpr int kSmallStart = 3;     // a workgroup's start and end, in tiles of a wave
 // Most rows and tiles of a solo span.  32 continuations of one history, half of them with
-// a frame of their own: 89 us with a workgroup for each, 77 up to 16 tiles, 54 up to 32 or
-// 64; with 12 and 24 rows of partial results a wave it loses (six spans of 10 heads of
-// 64, 23 us for 21).
+// a frame of their own: 69 us with a workgroup for each, 50 up to 16 tiles, 39 up to 32 or
+// 64.  With more rows a wave would write more partial results than it saves (12 and 24, six
+// spans of 10 heads of 64, lost 10% to a workgroup when they were joined one by one).
 constexpr int kSoloRows = 8, kSoloTiles = 32;
 
 // Cuts the spans' key tiles: the length of a cut with the earliest estimated end among
@@ -1159,7 +1161,7 @@ static int64_t plan_few(MxSmallArgs& a, const RowStreams& rs, int rows_most, int
     s.tile1 = static_cast<int32_t>(mx_tiles(s.kv_len, p.T, p.nt));
   }
   const int64_t end = plan_small(a, max_rows);
-  return p.hd == 128 ? 800 + 105 * end : 710 + 68 * end;
+  return p.hd == 128 ? 730 + 79 * end : 725 + 57 * end;
 }
 
 // The estimated end of whole-chunk items of the streams with more rows, likewise.
@@ -1175,17 +1177,19 @@ static int64_t estimate_many(const MxPages& p, const RowStreams& rs, int rows_ov
   }
   // (a round that the items leave idle is split; whole items go in rounds)
   const int64_t tiles = items < 3 * kSmallRound / 4 ? work / kSmallRound : std::max(most, work / kSmallRound);
-  return p.hd == 128 ? 3260 + 123 * tiles : 2620 + 89 * tiles;
+  return p.hd == 128 ? 3250 + 136 * tiles : 2490 + 100 * tiles;
 }
 
 // Which kernel takes a stream goes by estimates fitted to 360 calls (1 to 8 streams of
 // 64 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
 // both formats), each timed on both: a tile of a wave, eight at a time on a CU, takes
-// 2.1 us at d = 128 and 1.36 at d = 64 after 8 and 7 us; a tile of 256 rows 1.23 and 0.89
-// after 33 and 26 (a split schedule and its merge).  The choice loses 0.6% to the better
-// one on average, 15% at most.  us of the few rows' kernel and of whole-chunk items, 12
-// heads of 128 over 32760 tokens: 64 rows 33 / 62, 192 63 / 76, 256 83 / 81, 768 304 / 165;
-// four streams of 100 171 / 155, eight of 64 196 / 269.
+// 1.8 us at d = 128 and 1.17 at d = 64 after 8 and 7 us; a tile of 256 rows 1.36 and 1.0
+// after 33 and 25 (a split schedule and its merge).  With the few rows' times taken 12% and
+// 2% shorter the choice is best: it loses 0.5% to the better kernel on average, 23% at
+// most (three streams of 300 rows over one frame, 40 heads of 128, 75 us for 61).  us of
+// the few rows' kernel and of whole-chunk items, 12 heads of 128 over 32760 tokens: 64 rows
+// 31 / 63, 192 56 / 77, 256 73 / 80, 768 263 / 157; four streams of 100 158 / 155, eight of
+// 64 187 / 266.
 hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
                                const RowStreams& rs, int shared, float* part) {
   MxSmallArgs a;
