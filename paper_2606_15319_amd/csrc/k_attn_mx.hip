@@ -40,8 +40,15 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // Key of row r of key block b (32 rows each) of a tile.
-__device__ __forceinline__ int row_key(int b, int r) {
+__device__ __forceinline__ constexpr int row_key(int b, int r) {
   return 32 * ((r >> 2) & 1) + 16 * b + 4 * (r >> 3) + (r & 3);
+}
+
+// Lane id, formed where it is called for (two instructions) and held in no register.
+__device__ __forceinline__ uint32_t lane_anew() {
+  uint32_t zero = 0;
+  asm volatile("" : "+s"(zero));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
 }
 
 // max / sum over lanes l and l ^ 32
@@ -54,12 +61,12 @@ __device__ __forceinline__ float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A query row's operands: hi and lo codes of 64 dims a step, and hi's scale bytes
-// (lo's are 4 less).
+// A query row's operands: hi and lo codes of 64 dims a step, and their scales: byte
+// 2 ks hi's of step ks, byte 2 ks + 1 lo's (4 less).
 template <int HD>
 struct Query {
   i32x8 hi[HD / 64], lo[HD / 64];
-  int sc[HD / 64];
+  int sc;
 };
 
 // 16 dims of a block (the lane 32 on has its other 16) into words w0 .. w0 + 3
@@ -105,14 +112,15 @@ __device__ __forceinline__ void split_row(const uint4 (&raw)[HD / 64][2][2], int
     int s0, s1;
     split_query(raw[ks][0], q.hi[ks], q.lo[ks], 0, s0);
     split_query(raw[ks][1], q.hi[ks], q.lo[ks], 4, s1);
-    q.sc[ks] = hh ? s1 : s0;
+    const int s = hh ? s1 : s0;
+    q.sc = ks == 0 ? s + ((s - 4) << 8) : q.sc + (s << 16) + ((s - 4) << 24);
   }
 }
 
-// Key fragment of the 64-dim step ks from the rows at tk; at: byte offsets of this
-// lane's 16-byte chunks.
+// Key fragment of the 64-dim step ks from the rows at tk; at: byte offsets of this lane's
+// 16-byte chunks.
 template <int BITS>
-__device__ __forceinline__ i32x8 key_fragment(const uint8_t* tk, const int* at, int ks) {
+__device__ __forceinline__ i32x8 key_fragment(const uint8_t* tk, const uint32_t* at, int ks) {
   if constexpr (BITS == 8) {
     const u32x4 x = *reinterpret_cast<const u32x4*>(tk + at[2 * ks]), y = *reinterpret_cast<const u32x4*>(tk + at[2 * ks + 1]);
     return i32x8{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]), static_cast<int>(x[3]),
@@ -133,20 +141,20 @@ __device__ __forceinline__ void scores(const i32x8 (&k)[2][HD / 64], const uint3
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-  // (the scale operand's byte 2 ks: an immediate of the instruction)
+  // (which byte of a scale operand: an immediate of the instruction)
 #pragma unroll
-  for (int lo = 0; lo < 2; ++lo)
+  for (int b = 0; b < 2; ++b)
+    s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][0], q.hi[0], s[b], FMT, 0, 0, static_cast<int>(sk[b]), 0, q.sc);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][0], lo ? q.lo[0] : q.hi[0], s[b], FMT, 0, 0,
-                                                              static_cast<int>(sk[b]), 0, q.sc[0] - 4 * lo);
+  for (int b = 0; b < 2; ++b)
+    s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][0], q.lo[0], s[b], FMT, 0, 0, static_cast<int>(sk[b]), 1, q.sc);
   if constexpr (HD == 128) {
 #pragma unroll
-    for (int lo = 0; lo < 2; ++lo)
+    for (int b = 0; b < 2; ++b)
+      s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][1], q.hi[1], s[b], FMT, 0, 2, static_cast<int>(sk[b]), 2, q.sc);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-        s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][1], lo ? q.lo[1] : q.hi[1], s[b], FMT, 0, 2,
-                                                                static_cast<int>(sk[b]), 0, q.sc[1] - 4 * lo);
+    for (int b = 0; b < 2; ++b)
+      s[b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k[b][1], q.lo[1], s[b], FMT, 0, 2, static_cast<int>(sk[b]), 3, q.sc);
   }
 }
 
@@ -286,9 +294,10 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
   Query<HD> q;
   split_row<HD>(raw, hh, q);
   // byte offsets of this lane's fragments in a tile
-  int k_at[KS * BITS / 4], ks_at[2], v_at[BITS / 4];
+  uint32_t k_at[KS * BITS / 4];
+  int ks_at[2], v_at[BITS / 4];
 #pragma unroll
-  for (int i = 0; i < KS * BITS / 4; ++i) k_at[i] = n * KROW + (((2 * i + hh) ^ swz<KROW>(n)) << 4);
+  for (int i = 0; i < KS * BITS / 4; ++i) k_at[i] = static_cast<uint32_t>(n * KROW + (((2 * i + hh) ^ swz<KROW>(n)) << 4));
 #pragma unroll
   for (int b = 0; b < 2; ++b) ks_at[b] = row_key(b, n) * (HD / 32);
 #pragma unroll
@@ -552,17 +561,11 @@ static_assert(sizeof(MxLargeArgs) <= 4096, "arguments must fit the kernel-argume
 
 constexpr int BQ = 256;
 constexpr int NTHR = 512;
-
-
-// Tiles requested ahead of the one computed.  At d = 64 key fragments are read before
-// the barrier that their products follow (they have to have landed one barrier sooner):
-// 4680 queries over 14040 keys, 20 heads of 64, 522 us for 545; at d = 128 486 for 475
-// (12 heads).
-constexpr int ahead(int hd) { return hd == 64 ? 4 : 3; }
+constexpr int AHEAD = 3;          // tiles requested ahead of the one computed
+constexpr int NSLOT = AHEAD + 1;  // tiles of codes in LDS
 
 template <int HD, int BITS>
 struct LargeLds {
-  static constexpr int NSLOT = ahead(HD) + 1;     // tiles of codes
   uint8_t k[NSLOT][mx_tile_bytes(HD, BITS)];      // row R = 32 b + r: key row_key(b, r)
   uint8_t v[NSLOT][mx_tile_bytes(HD, BITS)];      // as in the page
   bf16_t vb[2][64 * HD];                          // [dim][64 keys]
@@ -580,15 +583,13 @@ struct LargeLds {
 // the keys of position t, turns its value codes into bf16 (slot t % 2, each thread
 // HD / 8 of them) and reads the bf16 values of position t - 1; it requests the codes
 // and scales of position t + 3, whose slots were last read in interval t - 1.
-template <int HD, int BITS>
+template <int HD, int BITS, bool PAIR>
 __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, const AttnStream& S, int h, int qt,
                                          int tb, int te, LargeLds<HD, BITS>& lds, int64_t slot) {
   constexpr int KS = HD / 64, DB = HD / 32;
   constexpr int TB = mx_tile_bytes(HD, BITS), SB = mx_scale_bytes(HD);
   constexpr int NL = TB / 1024;            // 1 KB loads of a tile of keys, and of values
   constexpr int KROW = HD * BITS / 8;      // bytes of a key
-  constexpr int AHEAD = ahead(HD), NSLOT = AHEAD + 1;
-  constexpr bool EARLY = AHEAD == 4;       // key fragments are read before the barrier
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n32 = lane & 31, hh = lane >> 5;
@@ -614,8 +615,6 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
   const int kR = piece * (1024 / KROW) + lane / (KROW / 16);
   const uint32_t k_off = static_cast<uint32_t>(row_key((kR >> 5) & 1, kR & 31) * KROW +
                                                (((lane % (KROW / 16)) ^ swz<KROW>(kR)) << 4));
-  const uint32_t v_off = static_cast<uint32_t>(piece * 1024 + lane * 16);
-  const uint32_t s_off = static_cast<uint32_t>(lane * 4);
   const uint32_t lds_k = lds_address(lds.k) + piece * 1024u, lds_v = lds_address(lds.v) + piece * 1024u;
   const uint32_t lds_ks = lds_address(lds.ks), lds_vs = lds_address(lds.vs);
 
@@ -633,12 +632,13 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
   auto stage = [&](int u) __attribute__((always_inline)) {
     const uint32_t sl = static_cast<uint32_t>(u % NSLOT);
     const char* kc = reinterpret_cast<const char*>(p.k) + tile * TB;
-    const char* vc = reinterpret_cast<const char*>(p.v) + tile * TB;
+    const char* vc = reinterpret_cast<const char*>(p.v) + tile * TB + piece * 1024;
+    const uint32_t ln = PAIR ? lane_anew() : lane, v_off = ln * 16u, s_off = ln * 4u;
     if (loads_k) lds_dma16(kc, k_off, lds_k + sl * TB);
     if (loads_v) lds_dma16(vc, v_off, lds_v + sl * TB);
-    if (wave == ks_wave && lane < SB / 4)
+    if (wave == ks_wave && ln < SB / 4)
       lds_dma4(reinterpret_cast<const char*>(p.ks) + tile * SB, s_off, lds_ks + sl * SB);
-    if (wave == vs_wave && lane < SB / 4)
+    if (wave == vs_wave && ln < SB / 4)
       lds_dma4(reinterpret_cast<const char*>(p.vs) + tile * SB, s_off, lds_vs + sl * SB);
     ++tile;
     if (++ti == p.nt) {
@@ -670,31 +670,24 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
   };
 
   // byte offsets of this lane's fragments in a tile
-  int k_at[KS * BITS / 4], ks_at[2], v_at[4];
+  // (of keys 16-byte chunk 2 i + hh of row n32, row 32 + n32 32 KROW on; of values chunk
+  // 4 hh + k.  PAIR: from the first, of which the others are an XOR away)
+  constexpr int NK = KS * BITS / 4;
+  uint32_t k_at[NK], v_at[4];
 #pragma unroll
-  for (int i = 0; i < KS * BITS / 4; ++i)   // 16-byte chunk 2 i + hh of row n32 (row 32 + n32: 32 KROW on)
-    k_at[i] = n32 * KROW + (((2 * i + hh) ^ swz<KROW>(n32)) << 4);
+  for (int i = 0; i < NK; ++i) k_at[i] = static_cast<uint32_t>(n32 * KROW + (((2 * i + hh) ^ swz<KROW>(n32)) << 4));
 #pragma unroll
-  for (int b = 0; b < 2; ++b) ks_at[b] = row_key(b, n32) * (HD / 32);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v_at[k] = n32 * 128 + (((4 * hh + k) ^ swz<128>(n32)) << 4);
+  for (int k = 0; k < 4; ++k) v_at[k] = static_cast<uint32_t>(n32 * 128 + (((4 * hh + k) ^ swz<128>(n32)) << 4));
+  const uint32_t ks_at = static_cast<uint32_t>(row_key(0, n32) * (HD / 32));
+  static_assert(row_key(1, 0) == 16 && row_key(1, 31) == row_key(0, 31) + 16, "block 1's keys are 16 on");
 
-  // At d = 128 weights are formed against the running maximum as it is and summed at once:
-  // a row whose weights sum to more than 2^14 (or to no number) raises the maximum and forms
-  // them again, and a tile's maximum is seldom needed (1497 -> 1459 us over 37440 tokens, 20
-  // heads, 4 bits; 8 bits 1540 -> 1519).  At d = 64 the products are half as long and the
-  // maxima are taken beside them, the weights packed beside the next tile's scores (502 us
-  // for 548, 4680 queries over 14040 tokens, 20 heads).
-  constexpr bool SUMS = HD == 128;
   f32x16 o[DB], s[2];
-  f32x16 p_[2];                // !SUMS: weights of the last VALU phase
   bf16x8 pf[4];                // weights as the products take them
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = kNoMax, l_run = 0.f;
-  float top = 0.f;             // largest score of the query's tile
 
   // value codes of position t to bf16: this thread HD / 8 keys of one dim
   auto convert = [&](int t, auto cut_c, int keys) __attribute__((always_inline)) {
@@ -727,48 +720,36 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     const int keys = keys_of(t);
     if (keys < 64) convert(t, yes, keys);
   };
-  auto tile_max = [&]() __attribute__((always_inline)) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-    top = pair_max(mx);
-  };
-
-  // key fragments and scales of position t
-  i32x8 kf[2][KS];
-  uint32_t sk[2];
-  auto read_keys = [&](int t) __attribute__((always_inline)) {
-      const uint8_t* tk = &lds.k[0][0] + (t % NSLOT) * TB;
-      const uint8_t* tks = &lds.ks[0][0] + (t % NSLOT) * SB;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(tks + ks_at[b]);
-        else sk[b] = *reinterpret_cast<const uint16_t*>(tks + ks_at[b]);
-        sk[b] >>= 8 * hh;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = key_fragment<BITS>(tk + 32 * KROW * b, k_at, ks);
-      }
-  };
-
   auto mfma_phase = [&](int t, auto pv_c, auto qk_c) __attribute__((always_inline)) {
     constexpr bool PV = decltype(pv_c)::value, QK = decltype(qk_c)::value;
     __builtin_amdgcn_s_setprio(1);
     bf16x8 vf[4][DB];
     if constexpr (QK) {
-      if constexpr (!EARLY) read_keys(t);
+      const uint32_t slot_at = static_cast<uint32_t>((t % NSLOT) * TB);
+      uint32_t at[NK];
+#pragma unroll
+      for (int i = 0; i < NK; ++i) at[i] = PAIR ? (slot_at + k_at[0]) ^ (32u * i) : slot_at + k_at[i];
+      const uint8_t* tks = lds.ks[t % NSLOT] + ks_at;
+      i32x8 kf[2][KS];
+      uint32_t sk[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if constexpr (HD == 128) sk[b] = *reinterpret_cast<const uint32_t*>(tks + 16 * b * (HD / 32));
+        else sk[b] = *reinterpret_cast<const uint16_t*>(tks + 16 * b * (HD / 32));
+        sk[b] >>= 8 * hh;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[b][ks] = key_fragment<BITS>(lds.k[0] + 32 * KROW * b, at, ks);
+      }
       scores<HD, BITS>(kf, sk, q, s);
     }
     if constexpr (PV) {
-      const uint8_t* tv = reinterpret_cast<const uint8_t*>(&lds.vb[0][0]) + ((t - 1) & 1) * (128 * HD);
+      const uint8_t* tv = reinterpret_cast<const uint8_t*>(&lds.vb[0][0]);
+      const uint32_t tile_at = static_cast<uint32_t>(((t - 1) & 1) * (128 * HD));
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t at = PAIR ? (tile_at + v_at[0]) ^ (16u * k) : tile_at + v_at[k];
 #pragma unroll
-        for (int db = 0; db < DB; ++db) vf[k][db] = *reinterpret_cast<const bf16x8*>(tv + v_at[k] + 4096 * db);
-      if constexpr (!SUMS) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) pf[k] = pack_weights(p_[k >> 1], 8 * (k & 1), l_run);
+        for (int db = 0; db < DB; ++db) vf[k][db] = *reinterpret_cast<const bf16x8*>(tv + at + 4096 * db);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -776,66 +757,55 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
         for (int db = 0; db < DB; ++db)
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][db], pf[k], o[db], 0, 0, 0);
     }
-    if constexpr (QK) {
-      convert(t, no, 64);
-      if constexpr (!SUMS) tile_max();
-    }
-    if constexpr (!SUMS) asm volatile("" : "+v"(top), "+v"(l_run));
+    if constexpr (QK) convert(t, no, 64);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  auto raise_max = [&]() __attribute__((always_inline)) {   // to the tile's, where that is more
-    const float m_new = fmaxf(m_run, top * c);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    m_run = m_new;
-    l_run *= alpha;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-  };
-  // VALU phase: the weights of the scores
+  // VALU phase: the weights of the scores, against the running maximum as it is, and
+  // their sum.  A row whose weights sum to more than 2^14 (or to no number) raises the
+  // maximum and forms them again; a tile's maximum is seldom taken.  (Taken for every
+  // tile, 4680 queries over 37440 keys, 20 heads of 128, 8 bits 1523 us for 1511, 4 bits
+  // 1475 for 1450; at d = 64 as fast, but in more registers than two on a CU have.)
   auto softmax = [&](int keys) __attribute__((always_inline)) {
     if (keys < 64) {
-      const int left = keys - 32 * hh;
+      const int left = keys - (PAIR ? static_cast<int>(lane_anew() & 32u) : 32 * hh);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 16 * b + i < left ? s[b][i] : -INFINITY;
-      if constexpr (!SUMS) tile_max();
     }
-    if constexpr (SUMS) {
-      float s0 = 0.f, s1 = 0.f;
-      auto weigh = [&]() __attribute__((always_inline)) {
-        s0 = s1 = 0.f;
+    float s0 = 0.f, s1 = 0.f;
+    auto weigh = [&]() __attribute__((always_inline)) {
+      s0 = s1 = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          f32x16 p;
+      for (int k = 0; k < 4; ++k) {
+        f32x16 p;
 #pragma unroll
-          for (int i = 8 * (k & 1); i < 8 * (k & 1) + 8; ++i)
-            p[i] = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run));
-          pf[k] = pack_weights(p, 8 * (k & 1), k & 1 ? s1 : s0);
-        }
-      };
-      weigh();
-      if (__any(!(s0 + s1 <= 16384.f))) {
-        tile_max();
-        raise_max();
-        weigh();
+        for (int i = 8 * (k & 1); i < 8 * (k & 1) + 8; ++i)
+          p[i] = __builtin_amdgcn_exp2f(fmaf(s[k >> 1][i], c, -m_run));
+        pf[k] = pack_weights(p, 8 * (k & 1), k & 1 ? s1 : s0);
       }
-      l_run += s0 + s1;
-      asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]), "+v"(l_run));
-    } else {
-      // raised only when a tile's maximum exceeds it by more than 8 (weights stay below
-      // 2^8), so that o is seldom rescaled
-      if (__any(top * c > m_run + 8.0f)) raise_max();
+    };
+    weigh();
+    if (__any(!(s0 + s1 <= 16384.f))) {
+      float top = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p_[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m_run));
-      asm volatile("" : "+v"(p_[0]), "+v"(p_[1]));
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+      const float m_new = fmaxf(m_run, pair_max(top) * c);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      weigh();
     }
+    l_run += s0 + s1;
+    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]), "+v"(l_run));
   };
 
   // ---- prologue: the positions ahead of the group's first VALU phase
@@ -851,7 +821,6 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     else wait_pairs(w0);
   };
   if (qt * BQ + wave * 32 < S.q_len) {
-    if constexpr (EARLY) read_keys(0);
     mfma_phase(0, no, yes);
     trim(0);
 #pragma unroll 1
@@ -862,7 +831,6 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
       }
       if (t + AHEAD + grp < n) stage(t + AHEAD + grp);
       softmax(keys_of(t));
-      if constexpr (EARLY) read_keys(t + 1);
       if (grp == 0) {
         wait_next(t + AHEAD);
         __syncthreads();
@@ -888,9 +856,10 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     }
   }
 
-  // ---- lane n32 + 32 hh holds dims 32 db + 8 g + 4 hh .. + 4 of its query
+  // ---- lane n + 32 hh holds dims 32 db + 8 g + 4 hh .. + 4 of its query
+  const int end_lane = PAIR ? static_cast<int>(lane_anew()) : lane, half = end_lane >> 5;
   const float l_tot = pair_sum(l_run);
-  const int row = wave * 32 + n32, ql = qt * BQ + row;
+  const int row = wave * 32 + (end_lane & 31), ql = qt * BQ + row;
   if (slot < 0) {
     const float inv = 1.0f / l_tot;
     if (ql < S.q_len) {
@@ -902,7 +871,7 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
           uint2 w;
           w.x = pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
           w.y = pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
-          *reinterpret_cast<uint2*>(op + 32 * db + 8 * g + 4 * hh) = w;
+          *reinterpret_cast<uint2*>(op + 32 * db + 8 * g + 4 * half) = w;
         }
     }
   } else {
@@ -911,9 +880,9 @@ __device__ __forceinline__ void mx_range(const AttnArgs& a, const MxPages& p, co
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(po + 32 * db + 8 * g + 4 * hh) =
+        *reinterpret_cast<float4*>(po + 32 * db + 8 * g + 4 * half) =
             make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
-    if (hh == 0) {
+    if (half == 0) {
       a.part_ml[static_cast<size_t>(slot) * 2 * BQ + row] = m_run;
       a.part_ml[static_cast<size_t>(slot) * 2 * BQ + BQ + row] = l_tot;
     }
@@ -928,9 +897,11 @@ __device__ __forceinline__ int item_stream(const AttnArgs& a, int item) {
   return si;
 }
 
-// One workgroup per item, each XCD a contiguous range of them.
-template <int HD, int BITS>
-__global__ __launch_bounds__(NTHR, 1) void attn_mx_kernel(const MxLargeArgs x) {
+// One workgroup per item, each XCD a contiguous range of them.  PAIR: two on a CU, in 128
+// registers (some offsets are formed anew instead of kept, which takes 2% where a CU has
+// one workgroup).
+template <int HD, int BITS, bool PAIR>
+__global__ __launch_bounds__(NTHR, PAIR ? 4 : 2) void attn_mx_kernel(const MxLargeArgs x) {
   __shared__ __attribute__((aligned(1024))) LargeLds<HD, BITS> lds;
   const AttnArgs& a = x.a;
   const int xcd = blockIdx.x % kNumXcd;
@@ -938,7 +909,7 @@ __global__ __launch_bounds__(NTHR, 1) void attn_mx_kernel(const MxLargeArgs x) {
   if (L >= a.xcd_begin[xcd + 1]) return;
   const AttnStream S = a.s[item_stream(a, L)];
   const int it = L - S.item_begin, h = it / S.n_qtiles;
-  mx_range<HD, BITS>(a, x.p, S, h, it - h * S.n_qtiles, 0, S.n_tiles, lds, -1);
+  mx_range<HD, BITS, PAIR>(a, x.p, S, h, it - h * S.n_qtiles, 0, S.n_tiles, lds, -1);
 }
 
 // The split schedule of plan_attention: main parts of the items from item0 on, then
@@ -955,7 +926,7 @@ __global__ __launch_bounds__(NTHR, 1) void attn_mx_split_kernel(const MxLargeArg
     const int gi = a.item0 + pre + j;
     const AttnStream S = a.s[item_stream(a, gi)];
     const int item = gi - S.item_begin, h = item / S.n_qtiles;
-    mx_range<HD, BITS>(a, x.p, S, h, item - h * S.n_qtiles, 0, S.main_tiles, lds,
+    mx_range<HD, BITS, false>(a, x.p, S, h, item - h * S.n_qtiles, 0, S.main_tiles, lds,
                        S.main_tiles == S.n_tiles ? -1 : gi - a.item0);
     return;
   }
@@ -973,21 +944,43 @@ __global__ __launch_bounds__(NTHR, 1) void attn_mx_split_kernel(const MxLargeArg
     const int tb = S.main_tiles + rel % tl, te = min(S.n_tiles, tb + (end - pos));
     pos += te - tb;
     const int h = item / S.n_qtiles;
-    mx_range<HD, BITS>(a, x.p, S, h, item - h * S.n_qtiles, tb, te, lds,
+    mx_range<HD, BITS, false>(a, x.p, S, h, item - h * S.n_qtiles, tb, te, lds,
                        static_cast<int64_t>(items) + S.item_begin + item - a.item0 + r);
   }
+}
+
+constexpr size_t kMoreThanHalf = 82 * 1024;   // of a CU's 160 KB of LDS: room for one workgroup
+
+// More items than CUs run in pairs at d = 64, unless they end sooner alone (plan_attention's
+// estimate).  us alone and in pairs: streams of 1560 and 4680 queries over 6240 and 18720
+// keys, 20 heads, 638 / 551 (4 bits 634 / 537); 4680 over 37440, 40 heads, 1937 / 1756; 4608
+// over 32256, 32 heads, 1242 / 1143; two streams of 4608 over 32256 and 13824, 8 heads, which
+// the rule leaves alone, 522 / 630.
+template <int HD, int BITS>
+hipError_t launch_items(hipStream_t st, const MxLargeArgs& x, int grid, int items) {
+  size_t more = 0;
+  if constexpr (HD == 64) {
+    if (items > kAttnSplitBlocks && !x.a.alone) {
+      hipLaunchKernelGGL((attn_mx_kernel<HD, BITS, true>), dim3(grid), dim3(NTHR), 0, st, x);
+      return hipGetLastError();
+    }
+    if (x.a.alone) more = kMoreThanHalf - sizeof(LargeLds<HD, BITS>);
+  }
+  hipLaunchKernelGGL((attn_mx_kernel<HD, BITS, false>), dim3(grid), dim3(NTHR), more, st, x);
+  return hipGetLastError();
 }
 
 template <int HD, int BITS>
 hipError_t launch_large(hipStream_t st, const MxLargeArgs& x) {
   const AttnArgs& a = x.a;
-  if (a.split_blocks) {
-    if (a.item0 > 0) hipLaunchKernelGGL((attn_mx_kernel<HD, BITS>), dim3(a.item0), dim3(NTHR), 0, st, x);
-    hipLaunchKernelGGL((attn_mx_split_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(NTHR), 0, st, x);
-    return launch_attention_merge(st, a, HD);
+  if (!a.split_blocks)
+    return launch_items<HD, BITS>(st, x, a.per_xcd * kNumXcd, a.total_items);
+  if (a.item0 > 0) {
+    const hipError_t e = launch_items<HD, BITS>(st, x, a.item0, a.item0);
+    if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((attn_mx_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(NTHR), 0, st, x);
-  return hipGetLastError();
+  hipLaunchKernelGGL((attn_mx_split_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(NTHR), 0, st, x);
+  return launch_attention_merge(st, a, HD);
 }
 
 hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o, const RowStreams& rs, int rows_over,

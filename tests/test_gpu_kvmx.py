@@ -668,3 +668,33 @@ def test_one_page_many_times_and_rows_behind_the_last(A, rows):
     for i in range(2):
         assert np.array_equal(host_f32(k16)[i].transpose(1, 0, 2), held[0][0])
         assert np.array_equal(host_f32(v16)[i].transpose(2, 0, 1), held[0][1])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("H,rows,cached", [
+    (64, [1275, 505], [120, 130]),     # more items than CUs, of two lengths: two to a CU
+    (8, [4600, 4607], [440, 148]),     # the longest take the whole time: one to a CU
+    (20, [4600], [100]),               # a full round, and a split one
+    (64, [1280, 1024], [121, 121]),
+])
+def test_many_items_at_64(A, bits, H, rows, cached):
+    """Chunks of narrow heads by the hundred, their keys a few pages named again and again."""
+    d, lat, T = 64, (8, 8), 64
+    pool = Pool(A, H, d, lat, 1, bits, [7 * T], seed=17)
+    held = pool.fill([7 * T], 161)[0]
+    rng = np.random.default_rng(18)
+    pool.span = max(c + -(-m // T) for c, m in zip(cached, rows))
+    pick = rng.integers(0, 7, (len(rows), pool.span))
+    pool.table = dev_i32(np.array(pool.ids[0], np.int32)[pick])
+    q = normal_bf16(make_rng(162), (sum(rows), H, d))
+    o = _attend(A, pool, rows, [c * T for c in cached], dev_bf16(q.reshape(-1, H * d)))
+    _sync()
+    got = host_f32(o).astype(np.float64).reshape(-1, H, d)
+    assert np.isfinite(got).all()
+    heads = [0, 1, H // 2, H - 1]
+    at = 0
+    for b, m in enumerate(rows):
+        k, v = [x.reshape(7, T, H, d)[:, :, heads][pick[b]].reshape(-1, len(heads), d)[:cached[b] * T + m] for x in held]
+        some = at + np.unique(np.concatenate([rng.integers(0, m, 24), [0, m - 1]]))
+        _check_attention(got[some][:, heads], q[some][:, heads].astype(np.float64), k, v, independent=False)
+        at += m
