@@ -220,19 +220,28 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
     Meeting<HD> part;
   } lds;
   const MxPages& p = a.p;
-  const int L = (static_cast<int>(blockIdx.x) % kNumXcd) * a.per_xcd + static_cast<int>(blockIdx.x) / kNumXcd;
-  if (L >= a.total_items) return;
+  const int xcd = static_cast<int>(blockIdx.x) % kNumXcd, j = static_cast<int>(blockIdx.x) / kNumXcd;
+  // first of a run's workgroups in the XCD's list
+  auto first = [&](const MxRun& r) { return r.eighths + r.rest / kNumXcd + (xcd < r.rest % kNumXcd ? 1 : 0); };
+  if (j >= first(a.run[a.n_runs])) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const bool solo = L >= a.solo_item;
-  const int item = solo ? (L - a.solo_item) * SM_WAVES + wave : L;
-  if (solo && item >= a.solo_waves) return;
-  // the last span that begins at or before the item: a lane looks at one of the others
-  // (one after the other they cost a scalar load and a wait each)
-  const int span0 = solo ? a.solo_span : 0, spans = (solo ? a.n_spans : a.solo_span) - span0;
-  const int si = span0 + __builtin_popcountll(__ballot(lane + 1 < spans &&
-                                                       item >= a.s[min(span0 + lane + 1, kMaxStreams)].item_begin));
+  // the last run that begins at or before the workgroup, and of solo spans the last that
+  // begins at or before the wave: a lane looks at one of the others (one after the other
+  // they cost a scalar load and a wait each)
+  const int e = __builtin_popcountll(__ballot(lane + 1 < a.n_runs && j >= first(a.run[min(lane + 1, a.n_runs)])));
+  const MxRun R = a.run[e], next = a.run[e + 1];
+  const int turn = (xcd - R.rest) & (kNumXcd - 1);   // the run's pieces begin with the XCD whose turn it is
+  int it = j - first(R) + turn * (next.eighths - R.eighths) + min(turn, next.rest - R.rest);
+  int si = a.run_span[e];
+  const bool solo = si >= a.solo_span;
+  if (solo) {
+    it = it * SM_WAVES + wave;
+    if (it >= a.solo_waves) return;
+    si += __builtin_popcountll(__ballot(si + lane + 1 < a.n_spans &&
+                                        it >= a.s[min(si + lane + 1, kMaxStreams)].wave_begin));
+  }
   const MxSpan S = a.s[__builtin_amdgcn_readfirstlane(si)];
-  const int it = item - S.item_begin;
+  if (solo) it -= S.wave_begin;
   const int hp = it / S.n_qtiles, qt = it - hp * S.n_qtiles;
   const int h = hp / S.pieces, piece = hp - h * S.pieces;
   const int tb = S.tile0 + piece * S.per_piece, te = min(S.tile1, tb + S.per_piece);
@@ -1010,7 +1019,9 @@ hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* 
 
 template <int HD, int BITS>
 hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
-  hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(a.per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
+  const MxRun& end = a.run[a.n_runs];
+  const int per_xcd = end.eighths + (end.rest + kNumXcd - 1) / kNumXcd;
+  hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
   if (a.join) {
     const int per = 256 / (HD / 4) / a.groups;   // rows of a workgroup
     hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + per - 1) / per), dim3(256), 0, st, a);
@@ -1093,15 +1104,26 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
     }
   }
   a.join = 0;
-  int64_t items = 0, rows = 0, solo = 0;
+  int64_t rows = 0, solo = 0;
+  int solo_longest = 0;
+  struct Run {
+    int span, cost;   // cost of a workgroup
+    int64_t wgs;
+  } runs[kMaxStreams + 1];
+  a.n_runs = 0;
   for (int i = 0; i < a.n_spans; ++i) {
     MxSpan& s = a.s[i];
     const int tiles = s.tile1 - s.tile0;
     s.pieces = cut(s, i, W);
     s.per_piece = (tiles + s.pieces - 1) / s.pieces;
-    int64_t& at = i < a.solo_span ? items : solo;
-    s.item_begin = static_cast<int32_t>(at);
-    at += static_cast<int64_t>(s.n_qtiles) * a.p.H * s.pieces;
+    const int64_t cuts = static_cast<int64_t>(s.n_qtiles) * a.p.H * s.pieces;
+    s.wave_begin = static_cast<int32_t>(solo);
+    if (i < a.solo_span) {
+      runs[a.n_runs++] = {i, kSmallStart + (s.per_piece + SM_WAVES - 1) / SM_WAVES, cuts};
+    } else {
+      solo += cuts;
+      solo_longest = std::max(solo_longest, kSmallStart + s.per_piece);
+    }
     s.part_begin = -1;
     if (s.pieces > 1 || a.shared) {
       s.part_begin = static_cast<int32_t>(rows);
@@ -1109,16 +1131,25 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
       a.join = 1;
     }
   }
+  if (solo) runs[a.n_runs++] = {a.solo_span, solo_longest, (solo + SM_WAVES - 1) / SM_WAVES};
+  a.solo_waves = static_cast<int32_t>(solo);
+  // Every XCD takes an eighth of each run in one piece (row tiles of the same keys meet in
+  // its L2), the longest workgroups first.  (In the batch's order, and each XCD a range of
+  // all: streams of 17, 192, 1, 700 and 65 rows over 62 to 404 tiles, 10 heads of 64, 54 us
+  // for 46; 32 continuations of one history 39 for 37.)
+  std::stable_sort(runs, runs + a.n_runs, [](const Run& x, const Run& y) { return x.cost > y.cost; });
+  a.run[0] = {0, 0};
+  for (int e = 0; e < a.n_runs; ++e) {
+    a.run_span[e] = static_cast<uint8_t>(runs[e].span);
+    a.run[e + 1].eighths = a.run[e].eighths + static_cast<int32_t>(runs[e].wgs / kNumXcd);
+    a.run[e + 1].rest = a.run[e].rest + static_cast<int32_t>(runs[e].wgs % kNumXcd);
+  }
   // groups of the join's lanes: four cuts each, of the row with most
   int cuts = 1;
   for (int i = a.shared; i < a.n_spans; ++i) cuts = std::max(cuts, a.s[i].pieces + (a.shared ? a.s[0].pieces : 0));
   const int lanes = a.p.hd / 4;
   a.groups = kWave / lanes;
   while (a.groups < 256 / lanes && 4 * a.groups < cuts) a.groups *= 2;
-  a.solo_item = static_cast<int32_t>(items);
-  a.solo_waves = static_cast<int32_t>(solo);
-  a.total_items = static_cast<int32_t>(items + (solo + SM_WAVES - 1) / SM_WAVES);
-  a.per_xcd = (a.total_items + kNumXcd - 1) / kNumXcd;
   return best;
 }
 

@@ -268,8 +268,13 @@ struct MxSpan {
   int32_t row;           // row of the page table
   int32_t tile0, tile1;
   int32_t n_qtiles, pieces, per_piece;   // row tiles; cuts of the key tiles, and tiles of a cut
-  int32_t item_begin;    // first workgroup, or of a solo span the first wave
+  int32_t wave_begin;    // of a solo span: its first wave
   int32_t part_begin;    // first partial row; -1: the output is written whole
+};
+// A run of workgroups is dealt to the XCDs, an eighth (rounded down) to each in one piece
+// and what is left one by one to the XCDs in turn: eighths and rests of the runs before it.
+struct MxRun {
+  int32_t eighths, rest;
 };
 struct MxSmallArgs {
   MxPages p;
@@ -279,9 +284,10 @@ struct MxSmallArgs {
   float scale_log2;      // log2(e) / sqrt(d)
   int32_t n_spans, shared;   // shared: span 0 is the common prefix, of all rows
   int32_t join, groups;  // some span leaves partial results; groups of lanes that join a row's
-  int32_t total_items, per_xcd;   // workgroups
-  int32_t solo_span;     // spans from here on: a cut is a wave's, not a workgroup's
-  int32_t solo_item, solo_waves;  // first workgroup of theirs, and their waves in all
+  int32_t solo_span, solo_waves;  // spans from here on, and their waves: a cut is a wave's
+  int32_t n_runs;        // workgroups of a span each, those of all solo spans one
+  MxRun run[kMaxStreams + 2];
+  uint8_t run_span[kMaxStreams + 1];
   int32_t rows;          // rows of the packed queries
   float* part_o;         // [partial rows][hd]
   float2* part_ml;       // [partial rows] running max, denominator
