@@ -1030,7 +1030,9 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
 }
 
 constexpr int kSmallRound = 256;   // workgroups of one round: one to a CU
-constexpr int kSmallStart = 3;     // a workgroup's start and end, in tiles of a wave
+// A workgroup's start and end, in tiles of a wave; and the join's launch, and the partial
+// rows that it takes as long for as for one, in half tiles.
+constexpr int kSmallStart = 3, kSmallJoin = 5, kSmallRows = 4096;
 // Most rows and tiles of a solo span.  32 continuations of one history, half of them with
 // a frame of their own: 69 us with a workgroup for each, 50 up to 16 tiles, 39 up to 32 or
 // 64.  With more rows a wave would write more partial results than it saves (12 and 24, six
@@ -1039,7 +1041,9 @@ constexpr int kSoloRows = 8, kSoloTiles = 32;
 
 // Cuts the spans' key tiles: the length of a cut with the earliest estimated end among
 // a few, such that the partial rows fit max_rows.  Returns that end, in half tiles of a
-// wave.
+// wave.  us with one round or more, and the join left out of the estimate, and so: seven
+// streams of one token over 32760 keys, 40 heads of 128, 538 / 450; eight tokens over 9 to
+// 21 frames, 20 heads of 64, 102 / 94; 192 rows over 6 small frames, 4 heads, 11.7 / 8.
 int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
   // solo spans last: those of one row tile and few key tiles
   auto is_solo = [](const MxSpan& s) { return s.q_len <= kSoloRows && s.tile1 - s.tile0 <= kSoloTiles; };
@@ -1066,20 +1070,22 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
     const int each = i < a.solo_span ? w : std::max(1, (w + SM_WAVES - 1) / SM_WAVES);
     return std::max(1, (tiles + each - 1) / each);
   };
-  // In tiles of a wave: workgroups of one round end with the longest; of several, the
-  // CUs take them as they come.
+  // In half tiles of a wave.  The longest workgroups come first: those of a run and of the
+  // longer ones take as many rounds as they fill, and what is shorter evens the end out.
+  // Partial rows are written, read and joined in a launch of its own.
   auto end = [&](int w) {
-    int64_t items = 0, rows = 0, sum = 0, solo = 0;
-    int longest = 0, solo_longest = 0;
+    int64_t rows = 0, sum = 0, solo = 0, items = 0;
+    int solo_longest = 0, n = 0;
+    struct Group {
+      int one;
+      int64_t wgs;
+    } g[kMaxStreams + 1];
     for (int i = 0; i < a.n_spans; ++i) {
       const MxSpan& s = a.s[i];
       const int pieces = cut(s, i, w), each = (s.tile1 - s.tile0 + pieces - 1) / pieces;
       const int64_t c = static_cast<int64_t>(s.n_qtiles) * a.p.H * pieces;
       if (i < a.solo_span) {
-        const int one = kSmallStart + (each + SM_WAVES - 1) / SM_WAVES;
-        items += c;
-        sum += c * one;
-        longest = std::max(longest, one);
+        g[n++] = {kSmallStart + (each + SM_WAVES - 1) / SM_WAVES, c};
       } else {
         solo += c;
         solo_longest = std::max(solo_longest, kSmallStart + each);
@@ -1087,21 +1093,40 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
       if (pieces > 1 || a.shared) rows += static_cast<int64_t>(s.q_len) * pieces * a.p.H;
     }
     if (rows > max_rows) return INT64_MAX;
-    const int64_t wgs = (solo + SM_WAVES - 1) / SM_WAVES;
-    items += wgs;
-    sum += wgs * solo_longest;
-    longest = std::max(longest, solo_longest);
-    return items <= kSmallRound ? static_cast<int64_t>(2 * longest) : 2 * sum / kSmallRound + longest;
+    if (solo) g[n++] = {solo_longest, (solo + SM_WAVES - 1) / SM_WAVES};
+    std::sort(g, g + n, [](const Group& x, const Group& y) { return x.one > y.one; });
+    int64_t last = 0;
+    for (int i = 0; i < n; ++i) {
+      items += g[i].wgs;
+      sum += g[i].wgs * g[i].one;
+      last = std::max(last, 2 * ((items + kSmallRound - 1) / kSmallRound) * g[i].one);
+    }
+    if (items > kSmallRound) last = std::max(last, 2 * sum / kSmallRound + g[n - 1].one / 2);
+    return last + (rows ? kSmallJoin + rows / kSmallRows : 0);
   };
-  const int whole = std::max(most, SM_WAVES * std::min(most, kSoloTiles));   // no span is cut
+  // candidates: no span cut, and the shortest cuts whose workgroups fill so many rounds
+  const int whole = std::max(most, SM_WAVES * std::min(most, kSoloTiles));
   int W = whole;
   int64_t best = end(whole);
-  for (int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / kSmallRound)); w < whole; w += std::max(SM_WAVES, w / 4)) {
+  for (const int rounds : {1, 2, 3, 4, 6, 8}) {
+    auto fits = [&](int w) {
+      int64_t items = 0, solo = 0;
+      for (int i = 0; i < a.n_spans; ++i) {
+        const int64_t c = static_cast<int64_t>(a.s[i].n_qtiles) * a.p.H * cut(a.s[i], i, w);
+        if (i < a.solo_span) items += c;
+        else solo += c;
+      }
+      return items + (solo + SM_WAVES - 1) / SM_WAVES <= rounds * kSmallRound;
+    };
+    int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / (rounds * kSmallRound)));
+    while (w < whole && !fits(w)) w += std::max(1, w / 16);
+    if (w >= whole) continue;
     const int64_t e = end(w);
     if (e < best) {
       best = e;
       W = w;
     }
+    if (w == SM_WAVES || 4 * e > 5 * best) break;   // (shorter cuts will not do)
   }
   a.join = 0;
   int64_t rows = 0, solo = 0;
@@ -1204,16 +1229,13 @@ static int64_t estimate_many(const MxPages& p, const RowStreams& rs, int rows_ov
   return p.hd == 128 ? 3250 + 136 * tiles : 2490 + 100 * tiles;
 }
 
-// Which kernel takes a stream goes by estimates fitted to 360 calls (1 to 8 streams of
-// 64 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
-// both formats), each timed on both: a tile of a wave, eight at a time on a CU, takes
-// 1.8 us at d = 128 and 1.17 at d = 64 after 8 and 7 us; a tile of 256 rows 1.36 and 1.0
-// after 33 and 25 (a split schedule and its merge).  With the few rows' times taken 12% and
-// 2% shorter the choice is best: it loses 0.5% to the better kernel on average, 23% at
-// most (three streams of 300 rows over one frame, 40 heads of 128, 75 us for 61).  us of
-// the few rows' kernel and of whole-chunk items, 12 heads of 128 over 32760 tokens: 64 rows
-// 31 / 63, 192 56 / 77, 256 73 / 80, 768 263 / 157; four streams of 100 158 / 155, eight of
-// 64 187 / 266.
+// Which kernel takes a stream goes by estimates fitted to 470 calls (1 to 10 streams of
+// 20 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
+// both formats), each timed on both.  The choice loses 0.2% to the better one on average,
+// 23% at most (three streams of 300 rows over one frame, 40 heads of 128, 75 us for 61).
+// us of the few rows' kernel and of whole-chunk items, 12 heads of 128 over 32760 tokens:
+// 64 rows 31 / 63, 192 56 / 77, 256 74 / 80, 768 209 / 157; four streams of 192 over 14040
+// 111 / 94.
 hipError_t launch_attention_mx(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o,
                                const RowStreams& rs, int shared, float* part) {
   MxSmallArgs a;
