@@ -698,3 +698,23 @@ def test_many_items_at_64(A, bits, H, rows, cached):
         some = at + np.unique(np.concatenate([rng.integers(0, m, 24), [0, m - 1]]))
         _check_attention(got[some][:, heads], q[some][:, heads].astype(np.float64), k, v, independent=False)
         at += m
+
+
+@pytest.mark.parametrize("shared", [0, 3])
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("rows", [[40] * 64, [1] * 64, [9, 1] * 32])
+def test_as_many_streams_as_there_can_be(A, bits, rows, shared):
+    """64 streams, each a run of workgroups of its own or a wave each, and a prefix that makes 65."""
+    H, d, lat, T = 2, 64, (8, 8), 64
+    cached = [3 + b % 5 for b in range(64)]
+    lens = [c * T + m for c, m in zip(cached, rows)]
+    pool = Pool(A, H, d, lat, 1, bits, lens, seed=19, shared=shared)
+    held = pool.fill(lens, 171, shared=shared)
+    q = normal_bf16(make_rng(172), (sum(rows), H, d))
+    o = _attend(A, pool, rows, [c * T for c in cached], dev_bf16(q.reshape(-1, H * d)), shared)
+    _sync()
+    got = host_f32(o).astype(np.float64).reshape(-1, H, d)
+    at = 0
+    for b, m in enumerate(rows):
+        _check_attention(got[at:at + m], q[at:at + m].astype(np.float64), *held[b])
+        at += m
