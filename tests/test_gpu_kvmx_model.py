@@ -121,3 +121,42 @@ def test_a_chunk_equals_its_passes(A, bits):
     for a, b in zip(*pools):
         for s, t in zip(a.dev, b.dev):
             assert np.array_equal(s.cpu().numpy(), t.cpu().numpy())
+
+
+def test_a_chunk_captured_and_replayed(A):
+    """Denoising and commit of a chunk in one graph, replayed on new inputs, against eager calls."""
+    import torch
+    n_layers, n_steps, ts = 2, [2, 1], [[1000.0, 500.0], [800.0]]
+    chunks = [2, 1]
+    m = Model(A, 92, n_layers, [20, 9])
+    lens, cached = [(c + 1) * LQ for c in chunks], [c * LQ for c in chunks]
+    pools = [_pool(A, SH, 8, lens, cached, 40 + l) for l in range(n_layers)]
+    batch = A.Batch([LQ] * 2, cached, [3 * c for c in chunks], m.ctx_lens)
+    ws, n = m.workspace(batch)
+    x = dev_bf16(normal_bf16(m.rng, (2 * LQ, SH.dim)))
+    noise = dev_bf16(normal_bf16(m.rng, (1, 2 * LQ, SH.dim)))
+    x0 = torch.empty((2 * LQ, SH.dim), dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        A.ardit_chunk_generate_mx(None, m.dims, batch, n_steps, ts, x, noise, [p.kv() for p in pools], m.tw,
+                                  m.ctx_k, m.ctx_v, m.w, x0, ws, n)
+
+    def state():
+        _sync()
+        return [host_bits(x0).copy()] + [t.cpu().numpy() for p in pools for t in p.dev]
+
+    step()
+    _sync()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(3):
+        x.copy_(dev_bf16(normal_bf16(m.rng, (2 * LQ, SH.dim))))
+        x0.fill_(float("nan"))
+        g.replay()
+        got = state()
+        assert np.isfinite(host_f32(x0)).all()
+        x0.fill_(float("nan"))
+        step()
+        for a, b in zip(got, state()):
+            assert np.array_equal(a, b)
