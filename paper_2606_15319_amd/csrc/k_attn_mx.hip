@@ -992,6 +992,37 @@ hipError_t launch_large(hipStream_t st, const MxLargeArgs& x) {
   return launch_attention_merge(st, a, HD);
 }
 
+// A round of equal items that leaves fewer CUs idle than plan_attention splits for: each
+// idle one takes the last tiles of k items, so many that it ends with the items; a piece
+// costs it `piece` 128ths of a tile more, all of them the merge (plan_attention's figures).
+// Taken from 3% on: the clock falls as more CUs are busy, and it gains half or less of what
+// the tiles say.  us whole and so: d = 128, 8 heads of 6240 queries (200 items, 319 tiles)
+// 490 / 434, 11 of 4680 (209, 299) 449 / 434, 12 (228, 299) 482 / 469, 524 tiles 796 / 792,
+// two streams of 6 heads 461 / 465; d = 64, 12 heads (228, 524) 555 / 526; not taken: 13
+// heads (247, 524) 830 / 847, 12 of 150 tiles 241 / 241.
+void shed_tails(AttnArgs& a, int head_dim, float* part) {
+  const int items = a.total_items, spare = kAttnSplitBlocks - items, n = a.s[0].n_tiles;
+  if (a.split_blocks || spare <= 0 || a.s[a.n_streams - 1].n_tiles != n) return;
+  const bool wide = head_dim == 128;
+  const int64_t piece = wide ? 640 : 320, k = (items + spare - 1) / spare;
+  const int64_t W = (k * (128 * static_cast<int64_t>(n) + piece) + 128 * (k + 1) - 1) / (128 * (k + 1));
+  const int64_t tl = n - W;
+  if (tl <= 0 || 128 * W + (wide ? 640 + 4 * items : 384 + 6 * items) >= 124 * static_cast<int64_t>(n)) return;
+  int64_t tails = 0;
+  for (int i = 0; i < a.n_streams; ++i) {
+    a.s[i].main_tiles = static_cast<int32_t>(W);
+    a.s[i].tail_begin = static_cast<int32_t>(tails);
+    tails += a.s[i].n_qtiles * a.H * tl;
+  }
+  a.item0 = 0;
+  a.split_blocks = kAttnSplitBlocks;
+  a.split_tiles = static_cast<int32_t>(k * tl);
+  a.total_tiles = static_cast<int32_t>(tails);
+  a.part_o = part;
+  a.part_ml = part + static_cast<size_t>(2) * kAttnSplitBlocks * BQ * head_dim;
+  a.per_xcd = kAttnSplitBlocks / kNumXcd;
+}
+
 hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* o, const RowStreams& rs, int rows_over,
                      float* part) {
   MxLargeArgs x;
@@ -1013,6 +1044,7 @@ hipError_t run_large(hipStream_t st, const MxPages& p, const bf16_t* q, bf16_t* 
     s.kv_len = static_cast<int32_t>(kAttnKTile * mx_tiles(s.base_off, p.T, p.nt));   // as planned: whole tiles
   }
   plan_attention(a, p.hd, part, false);
+  shed_tails(a, p.hd, part);
   if (p.hd == 128) return p.bits == 8 ? launch_large<128, 8>(st, x) : launch_large<128, 4>(st, x);
   return p.bits == 8 ? launch_large<64, 8>(st, x) : launch_large<64, 4>(st, x);
 }

@@ -718,3 +718,31 @@ def test_as_many_streams_as_there_can_be(A, bits, rows, shared):
     for b, m in enumerate(rows):
         _check_attention(got[at:at + m], q[at:at + m].astype(np.float64), *held[b])
         at += m
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("H,d,rows,cached", [
+    (12, 128, [4600], [200]),               # 216 items, six tails to each idle CU
+    (10, 128, [2300, 2290], [180, 180]),    # 180 of two streams
+    (12, 64, [4600], [260]),
+])
+def test_a_round_whose_items_shed_their_tails(A, bits, H, d, rows, cached):
+    """Items that leave a part of the CUs idle, their keys a few pages named again and again."""
+    lat, T = (8, 8), 64
+    pool = Pool(A, H, d, lat, 1, bits, [7 * T], seed=21)
+    held = pool.fill([7 * T], 181)[0]
+    rng = np.random.default_rng(22)
+    pool.span = max(c + -(-m // T) for c, m in zip(cached, rows))
+    pick = rng.integers(0, 7, (len(rows), pool.span))
+    pool.table = dev_i32(np.array(pool.ids[0], np.int32)[pick])
+    q = normal_bf16(make_rng(182), (sum(rows), H, d))
+    o = _attend(A, pool, rows, [c * T for c in cached], dev_bf16(q.reshape(-1, H * d)))
+    _sync()
+    got = host_f32(o).astype(np.float64).reshape(-1, H, d)
+    assert np.isfinite(got).all()
+    at = 0
+    for b, m in enumerate(rows):
+        k, v = [x.reshape(7, T, H, d)[pick[b]].reshape(-1, H, d)[:cached[b] * T + m] for x in held]
+        some = at + np.unique(np.concatenate([rng.integers(0, m, 16), [0, m - 1]]))
+        _check_attention(got[some], q[some].astype(np.float64), k, v, independent=False)
+        at += m
