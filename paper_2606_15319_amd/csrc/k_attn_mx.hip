@@ -995,11 +995,11 @@ hipError_t launch_large(hipStream_t st, const MxLargeArgs& x) {
 // A round of equal items that leaves fewer CUs idle than plan_attention splits for: each
 // idle one takes the last tiles of k items, so many that it ends with the items; a piece
 // costs it `piece` 128ths of a tile more, all of them the merge (plan_attention's figures).
-// Taken from 3% on: the clock falls as more CUs are busy, and it gains half or less of what
-// the tiles say.  us whole and so: d = 128, 8 heads of 6240 queries (200 items, 319 tiles)
-// 490 / 434, 11 of 4680 (209, 299) 449 / 434, 12 (228, 299) 482 / 469, 524 tiles 796 / 792,
-// two streams of 6 heads 461 / 465; d = 64, 12 heads (228, 524) 555 / 526; not taken: 13
-// heads (247, 524) 830 / 847, 12 of 150 tiles 241 / 241.
+// Taken where the tiles say 6% or more: the clock falls as more CUs are busy, and it gains
+// half of that or less.  us whole and so: d = 128, 8 heads of 6240 queries (200 items, 319
+// tiles) 490 / 434, 11 of 4680 (209, 299) 449 / 434, 12 (228, 524) 796 / 792; d = 64, 12
+// heads (228, 524) 555 / 526.  Not taken: 12 heads of 128 (228, 299; 4%) 461 / 465 to 482 /
+// 470 by the values held, 13 (247, 524) 830 / 847.
 void shed_tails(AttnArgs& a, int head_dim, float* part) {
   const int items = a.total_items, spare = kAttnSplitBlocks - items, n = a.s[0].n_tiles;
   if (a.split_blocks || spare <= 0 || a.s[a.n_streams - 1].n_tiles != n) return;
@@ -1007,7 +1007,7 @@ void shed_tails(AttnArgs& a, int head_dim, float* part) {
   const int64_t piece = wide ? 640 : 320, k = (items + spare - 1) / spare;
   const int64_t W = (k * (128 * static_cast<int64_t>(n) + piece) + 128 * (k + 1) - 1) / (128 * (k + 1));
   const int64_t tl = n - W;
-  if (tl <= 0 || 128 * W + (wide ? 640 + 4 * items : 384 + 6 * items) >= 124 * static_cast<int64_t>(n)) return;
+  if (tl <= 0 || 128 * W + (wide ? 640 + 4 * items : 384 + 6 * items) >= 120 * static_cast<int64_t>(n)) return;
   int64_t tails = 0;
   for (int i = 0; i < a.n_streams; ++i) {
     a.s[i].main_tiles = static_cast<int32_t>(W);
