@@ -1150,7 +1150,8 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
       }
       return items + (solo + SM_WAVES - 1) / SM_WAVES <= rounds * kSmallRound;
     };
-    int w = static_cast<int>(std::max<int64_t>(SM_WAVES, cost / (rounds * kSmallRound)));
+    // (a share of all tiles may pass the longest span, and 32 bits)
+    int w = static_cast<int>(std::clamp<int64_t>(cost / (rounds * kSmallRound), SM_WAVES, whole));
     while (w < whole && !fits(w)) w += std::max(1, w / 16);
     if (w >= whole) continue;
     const int64_t e = end(w);
