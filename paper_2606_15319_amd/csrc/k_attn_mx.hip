@@ -1008,6 +1008,7 @@ void shed_tails(AttnArgs& a, int head_dim, float* part) {
   const int64_t W = (k * (128 * static_cast<int64_t>(n) + piece) + 128 * (k + 1) - 1) / (128 * (k + 1));
   const int64_t tl = n - W;
   if (tl <= 0 || 128 * W + (wide ? 640 + 4 * items : 384 + 6 * items) >= 120 * static_cast<int64_t>(n)) return;
+  if (spare * k * tl > INT32_MAX) return;   // (the kernel counts the tails' tiles in 32 bits)
   int64_t tails = 0;
   for (int i = 0; i < a.n_streams; ++i) {
     a.s[i].main_tiles = static_cast<int32_t>(W);

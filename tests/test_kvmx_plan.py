@@ -68,3 +68,13 @@ def test_the_largest_calls_are_planned_in_time(plan, call):
     """Costs past 32 bits, and not a second of host time."""
     for w in plan([call], 5)[0]:
         assert w[2] != "few" or w[3][1:] == ["sound", "1"]
+
+
+@pytest.mark.parametrize("call", [f"128 8 {H} 32 0 1073733632,{q}" for H in (4, 5, 7, 8, 12) for q in (2000, 4096)]
+                         + ["64 4 9 96 0 1073741760,4096", "128 8 12 64 0 12800,4600", "128 8 11 1560 0 14040,4680"])
+def test_tails_are_counted_in_32_bits(plan, call):
+    """A round of few items over very many keys (half of every tile of 32-token pages is padding): every
+    tile is taken once, and no range of a split schedule passes 2^31."""
+    for w in plan([call])[0]:
+        if w[2] == "split":
+            assert int(w[3][1]) < 2 ** 31 and w[3][2:] == ["covered", "1"]
