@@ -490,7 +490,8 @@ __global__ __launch_bounds__(64 * SM_WAVES, 1) void attn_mx_small_kernel(const M
 }
 
 // Joins the partial results of a row: those of its stream's cuts and, when the batch
-// shares a prefix, of the prefix's.  HD / 4 lanes hold a row; a.groups such groups, at
+// shares a prefix, of the prefix's.  Rows that were written whole, or that are the other
+// kernel's, are not counted.  HD / 4 lanes hold a row; a.groups such groups, at
 // least a wave, take the cuts in turn and meet in LDS: one token over 32760 keys, one head,
 // 14 us for 16 with the groups of a wave (27 cuts: one group of lanes took 16 us for the
 // join alone, one trip to memory after the other, a wave of them 5).
@@ -502,14 +503,15 @@ __global__ __launch_bounds__(256) void attn_mx_join_kernel(const MxSmallArgs a) 
   const int grp = static_cast<int>(threadIdx.x) / TPR, c4 = threadIdx.x % TPR, lane = threadIdx.x & 63;
   const int sub = grp & (a.groups - 1);
   const int i = (static_cast<int>(blockIdx.x) * NG + grp) / a.groups;   // head-major rows, one to a wave
-  const int h = __builtin_amdgcn_readfirstlane(i / a.rows), r = __builtin_amdgcn_readfirstlane(i - h * a.rows);
+  const int h = __builtin_amdgcn_readfirstlane(i / a.join_rows), jr = __builtin_amdgcn_readfirstlane(i - h * a.join_rows);
   // the stream's span (in any order; each holds its rows once)
   const MxSpan& mine = a.s[min(a.shared + lane, kMaxStreams)];
-  const uint64_t hit = __ballot(a.shared + lane < a.n_spans && r >= mine.q_off && r - mine.q_off < mine.q_len);
+  const uint64_t hit = __ballot(a.shared + lane < a.n_spans && mine.part_begin >= 0 && jr >= mine.join_begin &&
+                                jr - mine.join_begin < mine.q_len);
   const int si = a.shared + (hit ? __builtin_ctzll(hit) : 0);
   const MxSpan S = a.s[__builtin_amdgcn_readfirstlane(si)];
-  // (a row of the other kernel's, or written whole: nothing to join)
-  const bool join = h < a.p.H && hit != 0 && S.part_begin >= 0;
+  const int r = S.q_off + jr - S.join_begin;
+  const bool join = h < a.p.H && hit != 0;
   const MxSpan& P = a.s[0];
   const int own = S.pieces, all = join ? own + (a.shared ? P.pieces : 0) : 0;
   float M = kNoMax, l = 0.f;
@@ -1055,9 +1057,9 @@ hipError_t launch_small(hipStream_t st, const MxSmallArgs& a) {
   const MxRun& end = a.run[a.n_runs];
   const int per_xcd = end.eighths + (end.rest + kNumXcd - 1) / kNumXcd;
   hipLaunchKernelGGL((attn_mx_small_kernel<HD, BITS>), dim3(per_xcd * kNumXcd), dim3(64 * SM_WAVES), 0, st, a);
-  if (a.join) {
+  if (a.join_rows) {
     const int per = 256 / (HD / 4) / a.groups;   // rows of a workgroup
-    hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.rows * a.p.H + per - 1) / per), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((attn_mx_join_kernel<HD>), dim3((a.join_rows * a.p.H + per - 1) / per), dim3(256), 0, st, a);
   }
   return hipGetLastError();
 }
@@ -1162,7 +1164,7 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
     }
     if (w == SM_WAVES || 4 * e > 5 * best) break;   // (shorter cuts will not do)
   }
-  a.join = 0;
+  a.join_rows = 0;
   int64_t rows = 0, solo = 0;
   int solo_longest = 0;
   struct Run {
@@ -1187,7 +1189,8 @@ int64_t plan_small(MxSmallArgs& a, int64_t max_rows) {
     if (s.pieces > 1 || a.shared) {
       s.part_begin = static_cast<int32_t>(rows);
       rows += static_cast<int64_t>(a.p.H) * s.pieces * s.q_len;
-      a.join = 1;
+      s.join_begin = a.join_rows;
+      if (i >= a.shared) a.join_rows += s.q_len;
     }
   }
   if (solo) runs[a.n_runs++] = {a.solo_span, solo_longest, (solo + SM_WAVES - 1) / SM_WAVES};

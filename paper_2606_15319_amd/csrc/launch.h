@@ -270,6 +270,7 @@ struct MxSpan {
   int32_t n_qtiles, pieces, per_piece;   // row tiles; cuts of the key tiles, and tiles of a cut
   int32_t wave_begin;    // of a solo span: its first wave
   int32_t part_begin;    // first partial row; -1: the output is written whole
+  int32_t join_begin;    // of partial results: its first row among those joined
 };
 // A run of workgroups is dealt to the XCDs, an eighth (rounded down) to each in one piece
 // and what is left one by one to the XCDs in turn: eighths and rests of the runs before it.
@@ -283,7 +284,7 @@ struct MxSmallArgs {
   int32_t ld;
   float scale_log2;      // log2(e) / sqrt(d)
   int32_t n_spans, shared;   // shared: span 0 is the common prefix, of all rows
-  int32_t join, groups;  // some span leaves partial results; groups of lanes that join a row's
+  int32_t join_rows, groups;  // rows with partial results; groups of lanes that join a row's
   int32_t solo_span, solo_waves;  // spans from here on, and their waves: a cut is a wave's
   int32_t n_runs;        // workgroups of a span each, those of all solo spans one
   MxRun run[kMaxStreams + 2];

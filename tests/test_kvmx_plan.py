@@ -78,3 +78,20 @@ def test_tails_are_counted_in_32_bits(plan, call):
     for w in plan([call])[0]:
         if w[2] == "split":
             assert int(w[3][1]) < 2 ** 31 and w[3][2:] == ["covered", "1"]
+
+
+@pytest.mark.parametrize("call,rows", [("64 8 128 64 0 0,1048576 640000,1", 1), ("64 4 64 64 0 0,2097152 64000,5 128000,3", 8),
+                                       ("128 8 12 1560 0 14040,4680 32760,1 9360,1", 2),
+                                       ("64 4 10 72 96 6912,3 7200,1 6984,24", 28)])
+def test_the_join_covers_the_rows_that_are_joined(plan, call, rows):
+    """A few rows beside very long streams: a launch holds fewer than 2^32 threads, and the join's
+    rows are those of the streams whose keys are cut."""
+    launches = plan([call])[0]
+    heads, lanes = int(call.split()[2]), int(call.split()[0]) // 4
+    assert launches[-1][2] == "join"
+    for wgs, threads, kernel, figures in launches:
+        assert wgs * threads < 2 ** 32
+        if kernel == "join":
+            assert int(figures[0]) == rows
+            per = 256 // lanes // int(figures[1])
+            assert wgs == -(-rows * heads // per)
