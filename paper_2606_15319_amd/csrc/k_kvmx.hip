@@ -56,14 +56,25 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t m) {   // over 4 neighbour
   return max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x4E, 0xf, 0xf, true)));
 }
 
+// fp64 to fp32 such that a rounding to fewer bits gives what it gives for x itself: the low
+// half of x is cut off and, where it held anything, the last bit that stays is set.  (21
+// bits stay, exact in fp32 down to 2^-129.)
+__device__ __forceinline__ float to_odd(double x) {
+  return static_cast<float>(__hiloint2double(__double2hiint(x) | static_cast<int>(min(static_cast<uint32_t>(__double2loint(x)), 1u)), 0));
+}
+
 // Queries and keys of RPW rows a wave.  Keys are normed and rotated in fp64 up to their
-// rounding to codes: a code's step is up to an eighth of its value, and with fp32's last
-// bits in doubt a few of seven million keys lie close enough to a border to take the other
-// code.  Rows of more than 1024 dims go one to a wave and wider ones to two or four waves,
-// so that a lane holds three or four pieces: fewer registers, more rows under way (with
-// their read-back, 4680 rows of 1536 29 us for 32 with two rows a wave, 9360 of 5120 169
-// for 186 with a wave each).  A lane holds chunks lane + 64 (part + WPR i) of 8 dims of a
-// row, so a block of 32 dims is four neighbouring lanes and a head 16 or 8 of them.
+// codes: a code's step is up to an eighth of its value, and with fp32's last bits in doubt 25
+// of sixteen million keys lie close enough to the border of two codes to take the farther
+// one.  Rounded to fp32 first, a key within 2^-25 of a border would come to lie on it, and 8
+// do so and go the wrong way: but all borders end in 19 zero bits, so the lanes that see
+// such a key, one in 2^16, form theirs again by to_odd (9360 rows of 5120, E4M3, 104 us for
+// 103; all keys by to_odd 112).  Rows of more than 1024 dims go one to a wave and wider ones
+// to two or four waves, so that a lane holds three or four pieces: fewer registers, more
+// rows under way (with their read-back, 4680 rows of 1536 29 us for 32 with two rows a wave,
+// 9360 of 5120 169 for 186 with a wave each).  A lane holds chunks lane + 64 (part + WPR i)
+// of 8 dims of a row, so a block of 32 dims is four neighbouring lanes and a head 16 or 8
+// of them.
 template <int MAXC, int RPW, int WPR, int BITS>
 __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, float* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -183,15 +194,24 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
         store_stream16(qo + c, pack8(y));
         unpack8(reinterpret_cast<const uint4*>(a.g_k)[c], g);
         unpack8(kraw[r][i], x);
-        uint32_t m = 0;
+        // largest of the lane's keys; least of their last 19 bits
+        uint32_t m, low;
+        auto turn = [&](auto to_fp32) {
+          m = 0;
+          low = ~0u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // (a product of two bf16 numbers is exact in fp32)
-          const double x0 = x[2 * e] * g[2 * e], x1 = x[2 * e + 1] * g[2 * e + 1];
-          y[2 * e] = static_cast<float>(rk * fma(x0, cc[e], -x1 * ss[e]));
-          y[2 * e + 1] = static_cast<float>(rk * fma(x0, ss[e], x1 * cc[e]));
-          m = max(m, max(__float_as_uint(y[2 * e]) & 0x7fffffffu, __float_as_uint(y[2 * e + 1]) & 0x7fffffffu));
-        }
+          for (int e = 0; e < 4; ++e) {
+            // (a product of two bf16 numbers is exact in fp32)
+            const double x0 = x[2 * e] * g[2 * e], x1 = x[2 * e + 1] * g[2 * e + 1];
+            y[2 * e] = to_fp32(rk * fma(x0, cc[e], -x1 * ss[e]));
+            y[2 * e + 1] = to_fp32(rk * fma(x0, ss[e], x1 * cc[e]));
+            const uint32_t u0 = __float_as_uint(y[2 * e]), u1 = __float_as_uint(y[2 * e + 1]);
+            m = max(m, max(u0 & 0x7fffffffu, u1 & 0x7fffffffu));
+            low = min(low, min(u0 & 0x7ffffu, u1 & 0x7ffffu));
+          }
+        };
+        turn([](double v) { return static_cast<float>(v); });
+        if (low == 0) turn(to_odd);   // one may be on a border that it was next to
         const int sb = mx_scale_byte<BITS>(quad_max(m));
         const uint2 w = mx_encode8<BITS>(y, mx_inverse(sb));
         // the scale bytes of a head meet in its first lane (a lane's own byte is that of
