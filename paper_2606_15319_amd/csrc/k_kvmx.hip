@@ -63,6 +63,8 @@ __device__ __forceinline__ float to_odd(double x) {
   return static_cast<float>(__hiloint2double(__double2hiint(x) | static_cast<int>(min(static_cast<uint32_t>(__double2loint(x)), 1u)), 0));
 }
 
+constexpr uint32_t kSmallKey = 67u << 23;   // bits of 2^-60
+
 // Queries and keys of RPW rows a wave.  Keys are normed and rotated in fp64 up to their
 // codes: a code's step is up to an eighth of its value, and with fp32's last bits in doubt 25
 // of sixteen million keys lie close enough to the border of two codes to take the farther
@@ -196,13 +198,15 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
         unpack8(kraw[r][i], x);
         // largest of the lane's keys; least of their last 19 bits
         uint32_t m, low;
-        auto turn = [&](auto to_fp32) {
+        auto turn = [&](auto wide, auto to_fp32) {
           m = 0;
           low = ~0u;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            // (a product of two bf16 numbers is exact in fp32)
-            const double x0 = x[2 * e] * g[2 * e], x1 = x[2 * e + 1] * g[2 * e + 1];
+            using P = decltype(wide);
+            if constexpr (sizeof(P) == 8) __builtin_amdgcn_sched_barrier(0);   // (one pair's registers at a time)
+            const double x0 = static_cast<P>(x[2 * e]) * static_cast<P>(g[2 * e]);
+            const double x1 = static_cast<P>(x[2 * e + 1]) * static_cast<P>(g[2 * e + 1]);
             y[2 * e] = to_fp32(rk * fma(x0, cc[e], -x1 * ss[e]));
             y[2 * e + 1] = to_fp32(rk * fma(x0, ss[e], x1 * cc[e]));
             const uint32_t u0 = __float_as_uint(y[2 * e]), u1 = __float_as_uint(y[2 * e + 1]);
@@ -210,8 +214,18 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int group, floa
             low = min(low, min(u0 & 0x7ffffu, u1 & 0x7ffffu));
           }
         };
-        turn([](double v) { return static_cast<float>(v); });
-        if (low == 0) turn(to_odd);   // one may be on a border that it was next to
+        // A product of two bf16 numbers is exact in fp32 between its ends: past the upper one a
+        // key is an infinity or NaN, which end in 19 zero bits too; below the lower one what is lost,
+        // 2^-150 rk, is nothing to keys of 2^-60 and more.
+        turn(0.0f, [](double v) { return static_cast<float>(v); });
+        if (low == 0 || m < kSmallKey || rk > 1024.0) {   // (on a border: maybe next to it)
+          uint4 k = kraw[r][i];
+          int again = c;   // (formed anew, so that nothing is held for the few that come here)
+          asm volatile("" : "+v"(k.x), "+v"(k.y), "+v"(k.z), "+v"(k.w), "+v"(again));
+          unpack8(reinterpret_cast<const uint4*>(a.g_k)[again], g);
+          unpack8(k, x);
+          turn(0.0, to_odd);
+        }
         const int sb = mx_scale_byte<BITS>(quad_max(m));
         const uint2 w = mx_encode8<BITS>(y, mx_inverse(sb));
         // the scale bytes of a head meet in its first lane (a lane's own byte is that of

@@ -46,11 +46,12 @@ def _near(rng, bits, border, delta, top):
     return row * rng.choice([-1.0, 1.0], D)
 
 
-def _append(A, bits, qkv, gain):
+def _append(A, bits, qkv, gain, eps=EPS):
     """Keys of one stream of frames of 8 x 8 tokens, two heads of 64, from position 0: what its pages hold, and the pool."""
     import torch
     n, H, d, T = len(qkv), 2, 64, 64
     pool = Pool(A, H, d, (8, 8), 1, bits, [T] * (n // T), fill=0)
+    pool.dims = A.make_dims(H * d, H, d, 128, 1, 8, 8, eps)
     pool.upload()
     q = torch.empty((n, H * d), dtype=torch.bfloat16, device="cuda")
     B = n // T
@@ -61,9 +62,9 @@ def _append(A, bits, qkv, gain):
     return np.concatenate([pool.host.unpack(i[0])[0] for i in pool.ids]), q
 
 
-def _want(rows, gain):
+def _want(rows, gain, eps=EPS):
     """Keys of _append in 64 bits."""
-    k = O.rms_norm(rows.astype(np.float64), EPS, gain.astype(np.float64)).reshape(-1, 2, 64)
+    k = O.rms_norm(rows.astype(np.float64), eps, gain.astype(np.float64)).reshape(-1, 2, 64)
     return np.concatenate([O.rope3d(k[t:t + 64], O.chunk_positions(1, 8, 8, 0), 10000.0) for t in range(0, len(k), 64)])
 
 
@@ -123,3 +124,38 @@ def test_every_key_takes_the_nearest_code(A, bits, H, d, lat):
         kr = O.rope3d(O.rms_norm(x, EPS, host_f32(g)).reshape(T, H, d), O.chunk_positions(1, *lat, pos), 10000.0)
         got = pool.host.unpack(pool.ids[b][0])[0]
         assert np.all(np.abs(got - kr) - np.abs(M.rounded(kr, bits, -1) - kr) <= 1e-12)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_projections_at_the_end_of_bf16(A, bits):
+    """Keys of a usual size from projections near the largest bf16 number, whose product with the gain, as their
+    square, is past fp32."""
+    rng = np.random.default_rng(211)
+    qkv = normal_bf16(make_rng(212), (64, 3 * 128)).astype(np.float32)
+    rows = _bf16(rng.standard_normal((64, 128)).astype(np.float32))
+    rows[::2] *= np.float32(2.0 ** 125)
+    rows[5] = 0
+    rows[5, 2] = -1.5 * 2.0 ** 127
+    rows[7] = 2.0 ** 127
+    qkv[:, 128:256] = rows
+    gain = np.where(np.arange(128) % 2, 1.75, 3.0).astype(np.float32)
+    kr = _want(rows, gain)
+    assert np.isfinite(rows).all() and np.abs(kr).max() < 40
+    got, q = _append(A, bits, qkv, gain)
+    assert np.isfinite(host_f32(q)).all()
+    assert np.all(np.abs(got - kr) - np.abs(M.rounded(kr, bits, -1) - kr) <= 1e-12)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_projections_at_bf16s_small_end(A, bits):
+    """Subnormal projections whose product with the gain is less than fp32 holds to its last bit, over a small eps."""
+    rng = np.random.default_rng(213)
+    qkv = normal_bf16(make_rng(214), (64, 3 * 128)).astype(np.float32)
+    rows = np.ldexp(rng.integers(-127, 128, (64, 128)).astype(np.float32), -133)
+    qkv[:, 128:256] = rows
+    gain = _bf16(rng.uniform(1, 2, 128) * 2.0 ** -14)
+    eps = float(np.float32(1e-36))
+    kr = _want(rows, gain, eps)
+    assert 2.0 ** -90 < np.abs(kr).max() < 2.0 ** -70
+    got, _ = _append(A, bits, qkv, gain, eps)
+    assert np.array_equal(got, M.rounded(kr, bits, -1))
