@@ -304,13 +304,15 @@ int ardit_kv_read_mx(hipStream_t stream, const ardit_dims* dims, const ardit_bat
                      const ardit_kv_mx* src, const ardit_kv_paged* dst);
 
 /* ardit_attn_fwd over a microscaled cache: o = softmax(q K^T / sqrt(d)) V with K, V
- * the values the codes stand for and q in bf16, not quantised; any q_lens.  All
- * streams bf16 and dense (batch->quant and batch->sparsity: ARDIT_EUNSUPPORTED
- * otherwise).  shared_frames > 0 says that the batch continues one history: the
- * first shared_frames table entries of every stream that has queries are the
- * same (with ardit_debug_checks(1) ARDIT_EINVAL otherwise), and each such stream
- * caches at least those frames (ARDIT_ESHAPE); their pages are then read once for the rows
- * of all streams where that saves work.  Few rows are split over their keys, and
+ * the values the codes stand for and q in bf16, not quantised; any q_lens.  Scores,
+ * maximum and denominator are fp32; the weights are rounded to bf16 for the product
+ * with V, as in ardit_attn_fwd (2.3e-3 of an output in all, where the rounding of o
+ * alone is 1.7e-3).  All streams bf16 and dense (batch->quant and batch->sparsity:
+ * ARDIT_EUNSUPPORTED otherwise).  shared_frames > 0 says that the batch continues one
+ * history: the first shared_frames table entries of every stream that has queries are
+ * the same (with ardit_debug_checks(1) ARDIT_EINVAL otherwise), and each such stream
+ * caches at least those frames (ARDIT_ESHAPE); their pages are then read once for the
+ * rows of all streams where that saves work.  Few rows are split over their keys, and
  * the schedule depends on the whole batch, as in ardit_attn_fwd.  ws / ws_bytes:
  * ardit_workspace_size of this batch. */
 int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,

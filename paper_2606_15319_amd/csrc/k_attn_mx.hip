@@ -965,8 +965,8 @@ constexpr size_t kMoreThanHalf = 82 * 1024;   // of a CU's 160 KB of LDS: room f
 // More items than CUs run in pairs at d = 64, unless they end sooner alone (plan_attention's
 // estimate).  us alone and in pairs: streams of 1560 and 4680 queries over 6240 and 18720
 // keys, 20 heads, 638 / 551 (4 bits 634 / 537); 4680 over 37440, 40 heads, 1937 / 1756; 4608
-// over 32256, 32 heads, 1242 / 1143; two streams of 4608 over 32256 and 13824, 8 heads, which
-// the rule leaves alone, 522 / 630.
+// over 32256, 32 heads, 1242 / 1143; two streams of 4608 over 32256 and 13824, 8 heads, 522 /
+// 630, which the rule would leave alone (the few rows' kernel has them, see below).
 template <int HD, int BITS>
 hipError_t launch_items(hipStream_t st, const MxLargeArgs& x, int grid, int items) {
   size_t more = 0;
@@ -1266,10 +1266,14 @@ static int64_t estimate_many(const MxPages& p, const RowStreams& rs, int rows_ov
   return p.hd == 128 ? 3250 + 136 * tiles : 2490 + 100 * tiles;
 }
 
-// Which kernel takes a stream goes by estimates fitted to 470 calls (1 to 10 streams of
+// Which kernel takes a stream goes by estimates fitted to 468 calls (1 to 10 streams of
 // 20 to 768 rows over 1 to 21 frames of 1560 tokens, 4, 12 and 40 heads of 64 and 128,
-// both formats), each timed on both.  The choice loses 0.2% to the better one on average,
-// 23% at most (three streams of 300 rows over one frame, 40 heads of 128, 75 us for 61).
+// both formats), each timed on both.  The choice loses 0.5% to the better one on average,
+// 26% at most (three streams of 300 rows over one frame, 40 heads of 128, 78 us for 62).
+// Streams of 780 to 4680 rows in 36 calls that it gives to the few rows' kernel: from half
+// the time of whole-chunk items (3120 rows over 3 frames beside 780 over 18, 16 heads of 128,
+// 357 / 646) to 14% more (4680 over 21 and 780 over 22, 10 heads of 64, 650 / 568), 2% lost
+// on average.
 // us of the few rows' kernel and of whole-chunk items, 12 heads of 128 over 32760 tokens:
 // 64 rows 31 / 63, 192 56 / 77, 256 74 / 80, 768 209 / 157; four streams of 192 over 14040
 // 111 / 94.
