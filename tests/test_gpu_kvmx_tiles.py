@@ -13,6 +13,24 @@ from workloads import make_rng, normal_bf16
 pytestmark = pytest.mark.gpu
 
 T = 64
+# the weights and their sum 2^-8 each, the store 2^-8, scores and exp2 2^-10
+BOUND = 3 * 2.0 ** -8 + 2.0 ** -10
+
+
+def times(d, table, n):
+    """How often each key of each of the d pages is among the first n keys of a table of pages."""
+    count = np.zeros((d, T))
+    np.add.at(count, table[:n // T], 1.0)
+    if n % T:
+        count[table[n // T], :n % T] += 1.0
+    return count
+
+
+def page_weights(q, keys, count):
+    """What rows q [m, d] give to each page: keys [pages, T, d] of one head, attended to `count` times each."""
+    s = q @ keys.reshape(-1, q.shape[-1]).T / np.sqrt(q.shape[-1])
+    p = (np.exp(s - s.max(-1, keepdims=True)) * count.reshape(-1)).reshape(len(q), *count.shape)
+    return p.sum(-1) / p.sum((-2, -1))[:, None]
 
 
 @pytest.fixture(scope="module")
@@ -51,19 +69,13 @@ def _check(A, H, d, bits, rows, cached, shared=0):
     at = 0
     for b, m in enumerate(rows):
         n = cached[b] * T + m
-        # how often each key of each page is attended to
-        count = np.zeros((d, T))
-        np.add.at(count, pick[b, :n // T], 1.0)
-        count[pick[b, n // T] if n % T else 0, :n % T] += 1.0
+        count = times(d, pick[b], n)
         assert count.sum() == n
         # rows of every 256-row tile, and the last
         some = [at + int(rng.integers(r, min(r + 256, m))) for r in range(0, m, 256)] + [at + m - 1] if m else []
         for h in range(H):
-            s = q[some, h].astype(np.float64) @ keys[:, :, h].reshape(-1, d).T / np.sqrt(d)
-            p = (np.exp(s - s.max(-1, keepdims=True)) * count.reshape(-1)).reshape(-1, d, T)
-            ref = p.sum(-1) / p.sum((-2, -1))[:, None]
-            # (the weights and their sum 2^-8 each, the store 2^-8, scores and exp2 2^-10)
-            assert np.all(np.abs(got[some, h] - ref) <= (3 * 2.0 ** -8 + 2.0 ** -10) * ref), h
+            ref = page_weights(q[some, h].astype(np.float64), keys[:, :, h], count)
+            assert np.all(np.abs(got[some, h] - ref) <= BOUND * ref), h
         at += m
 
 
