@@ -1,4 +1,4 @@
-// Host-only driver of the microscaled attention's planning: launches are recorded here
+// Runs, on the host alone, the microscaled attention's planning: launches are recorded here
 // instead of reaching a GPU, and the split schedule's index arithmetic is followed in 64
 // bits.  Each argument is a call, "hd bits H T shared cached,q cached,q ...", and gives a
 // line of its launches, and the status:
