@@ -280,15 +280,15 @@ def run(state):
         p = s["plan"]
         A = p["A"]
         if op == "linear":
-            A.ardit_linear_i8(None, p["desc"], p["y"], p["out"], s["case"]["n"])
+            A.ardit_int_linear(None, p["desc"], p["y"], p["out"], s["case"]["n"])
             return p["y"]
         if op == "quantize":
-            A.ardit_quantize_rows_i8(None, s["x"], p["type"], p["rows"], p["cols"], s["x"].stride(0), p["codes"],
-                                     p["codes"].stride(0), p["scales"])
+            A.ardit_int_quantize(None, s["x"], p["type"], p["rows"], p["cols"], s["x"].stride(0), p["codes"],
+                                 p["codes"].stride(0), p["scales"])
         else:
-            A.ardit_norm_quantize_i8(None, p["rows"], p["cols"], p["desc"], p["codes"], p["codes"].stride(0), p["scales"])
-        A.ardit_dequantize_rows_i8(None, p["codes"], p["rows"], p["cols"], p["codes"].stride(0), p["scales"], p["values"],
-                                   A.F32, p["cols"])
+            A.ardit_int_norm(None, p["rows"], p["cols"], p["desc"], p["codes"], p["codes"].stride(0), p["scales"])
+        A.ardit_int_dequantize(None, p["codes"], p["rows"], p["cols"], p["codes"].stride(0), p["scales"], p["values"],
+                               A.F32, p["cols"])
         out = {"values": p["values"], "scales": p["scales"]}
         if p.get("h") is not None:
             out["h"] = p["h"]
