@@ -319,6 +319,104 @@ int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_ba
                       const void* q, const ardit_kv_mx* kv, int32_t shared_frames, void* o, void* ws,
                       size_t ws_bytes);
 
+/* ---- Linear layers in 8-bit integers.
+ * A row of int8 codes q_j has one fp32 scale s and stands for q_j s.  Codes of a row y,
+ * with m = max_j |y_j|: s = fl32(m / 127) and q_j the whole number nearest to 127 y_j / m,
+ * ties to even, decided exactly (up to fp64 where y is itself computed), so |q_j| <= 127 and
+ * the largest element has 127.  m = 0 gives s = 0 and zeros.  A row that holds an infinity or
+ * a NaN gets s = NaN and zero codes: it reads back, and goes through a product, as NaN.  (For
+ * m below 2^-119 s is subnormal and holds fewer bits.)
+ * Rows of codes are 16-byte aligned and ldc (a multiple of 16, at least cols) bytes apart; the
+ * calls that write codes write zeros from cols up to the next multiple of 16 and nothing past
+ * that.  Zero rows (and only then NULL buffers) are allowed: nothing is done.  Rows of other
+ * tensors may start anywhere an element may (16-byte aligned bases with strides of 16 bytes
+ * run faster); strides are in elements and at least the row's length. */
+
+/* Element type of a tensor argument. */
+typedef enum { ARDIT_BF16 = 0, ARDIT_F32 = 1 } ardit_type;
+
+/* Rows of x (device, x_type, row stride ldx) to codes (device int8 [rows][ldc]) and scales
+ * (device fp32 [rows]): weights once (a scale per output channel), activations online (a scale
+ * per token).  1 <= cols <= 65536, rows <= 2^22. */
+int ardit_int_quantize(hipStream_t stream, const void* x, int32_t x_type, int64_t rows, int32_t cols,
+                       int64_t ldx, void* codes, int64_t ldc, float* scales);
+
+/* Codes back: y = fl32(q s), in bf16 that rounded again (device, row stride ldy). */
+int ardit_int_dequantize(hipStream_t stream, const void* codes, int64_t rows, int32_t cols,
+                         int64_t ldc, const float* scales, void* y, int32_t y_type, int64_t ldy);
+
+/* What ardit_int_norm computes for a row (host struct, device pointers), b = row / rows_per_stream:
+ *   V_r = fl32(mod[b][r] + mod_table[r]) for the rows r named below (mod_table NULL: mod[b][r])
+ *   h   = x, or with delta fl32(x + V_gate delta) (gate_row -1: x + delta), rounded once
+ *   u   = h / sqrt(mean(h^2) + eps)
+ *   y   = u * gain  |  u * (1 + V_scale) + V_shift (scale_row or shift_row -1: without)  |  u
+ * and the codes of y.  (In a block: the gated residual's addition and adaLN, or the
+ * cross-attention's pre-norm.)  Sums are fp64, codes exact as above. */
+typedef struct {
+  const void* x;            /* [rows][dim], x_type, stride ldx: the residual stream */
+  int32_t x_type;
+  int64_t ldx;
+  const void* delta;        /* [rows][dim], delta_type, stride ldd: the branch added, or NULL */
+  int32_t delta_type;
+  int64_t ldd;
+  float* h;                 /* [rows][dim] fp32, stride ldh: the sum kept, or NULL.  May be x or
+                               delta itself (fp32, same stride); no other overlap with them */
+  int64_t ldh;
+  const void* gain;         /* [dim] bf16, or NULL; not together with shift_row or scale_row */
+  const float* mod;         /* [ceil(rows / rows_per_stream)][6][dim], or NULL where no row is named */
+  const float* mod_table;   /* [6][dim], or NULL */
+  int32_t shift_row, scale_row, gate_row;   /* 0 .. 5, or -1 for none */
+  int64_t rows_per_stream;  /* >= 1; read where a row is named */
+  double eps;               /* > 0 */
+} ardit_norm_desc;
+
+/* The norm of a linear layer's input with the residual's addition before it and its output in
+ * codes (device int8 [rows][ldc]) and scales (device fp32 [rows]).  1 <= dim <= 8192,
+ * rows <= 2^22. */
+int ardit_int_norm(hipStream_t stream, int64_t rows, int32_t dim, const ardit_norm_desc* norm,
+                   void* codes, int64_t ldc, float* scales);
+
+/* What follows a product of codes. */
+typedef enum { ARDIT_ACT_NONE = 0, ARDIT_ACT_GELU = 1 } ardit_act;
+
+/* A linear layer over codes (host struct, device pointers): with b = row / rows_per_stream,
+ *   z = (sum_k x_codes[i][k] w_codes[j][k]) x_scales[i] w_scales[j] + bias[j]
+ *   y = z  |  GELU_tanh(z)  |  res + z  |  res + fl32(mod[b][gate_row] + mod_table[gate_row]) z
+ * The sum is exact (32-bit integers: k <= 65536), what follows fp32, y rounded once.  Where k is
+ * not a multiple of 16, each row of both goes on to the next multiple and one of the two holds
+ * zeros there (the calls above leave zeros in both).  A row depends on no other row: it has the
+ * same bits in any batch. */
+typedef struct {
+  int32_t m, n, k;          /* m rows (0 .. 2^22) to n outputs (1 .. 2^20) over k (1 .. 65536) */
+  const void* x_codes;      /* int8 [m][ldx] */
+  int64_t ldx;
+  const float* x_scales;    /* [m] */
+  const void* w_codes;      /* int8 [n][ldw] ([out][in], as every weight) */
+  int64_t ldw;
+  const float* w_scales;    /* [n] */
+  const void* bias;         /* bf16 [n], or NULL */
+  int32_t act;              /* ardit_act; ARDIT_ACT_GELU without a residual and with y in bf16 */
+  const void* res;          /* [m][n], res_type, stride ldr, or NULL.  May be y itself (same type
+                               and stride); no other overlap */
+  int32_t res_type;
+  int64_t ldr;
+  const float* mod;         /* [ceil(m / rows_per_stream)][6][n] with gate_row, else NULL */
+  const float* mod_table;   /* [6][n], or NULL */
+  int32_t gate_row;         /* 0 .. 5 (needs res), or -1 */
+  int64_t rows_per_stream;  /* >= 1; read with gate_row */
+} ardit_linear_desc;
+
+/* y (device, y_type, row stride ldy) of the layer above. */
+int ardit_int_linear(hipStream_t stream, const ardit_linear_desc* linear, void* y, int32_t y_type,
+                     int64_t ldy);
+
+/* The six weight matrices of a block in codes (device int8, [out][in] without padding between
+ * rows: dim and ffn_dim are multiples of 128) with a scale per output channel (device fp32). */
+typedef struct {
+  const void *w_qkv, *w_o, *w_cq, *w_co, *w_1, *w_2;
+  const float *s_qkv, *s_o, *s_cq, *s_co, *s_1, *s_2;
+} ardit_block_weights_int;
+
 /* Block selection of block-sparse self-attention (paper, Section 2.1: the
  * sparsity knob rho skips attention blocks a sparse mask leaves out; Section 5
  * names Light Forcing as the method, whose rule the paper does not give).
@@ -380,6 +478,17 @@ int ardit_stack_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_b
                        int32_t n_layers, const void* x, const ardit_kv_mx* kv, const float* mod,
                        const void* const* ctx_k, const void* const* ctx_v,
                        const ardit_block_weights* w, void* out, void* ws, size_t ws_bytes);
+
+/* ardit_stack_fwd with the six linears of every block in 8-bit integers: w8 (host array of
+ * n_layers) gives their matrices, w everything else (its matrices w_qkv, w_o, w_cq, w_co, w_1 and
+ * w_2 are not read and may be NULL).  The inputs of the linears are quantised per token: the
+ * norms' outputs from fp32, attention and GELU outputs from bf16; the text keys and values come
+ * from ardit_ctx_kv as before.  batch->sparsity and batch->quant apply. */
+int ardit_stack_fwd_int(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                        int32_t n_layers, const void* x, const ardit_kv_paged* kv, const float* mod,
+                        const void* const* ctx_k, const void* const* ctx_v,
+                        const ardit_block_weights* w, const ardit_block_weights_int* w8, void* out,
+                        void* ws, size_t ws_bytes);
 
 /* Page table of one stream under a sink + sliding-window cache (paper,
  * Section 2.1: the cache keeps a few sink chunks plus the most recent W
@@ -450,6 +559,15 @@ int ardit_chunk_generate_mx(hipStream_t stream, const ardit_dims* dims, const ar
                             const void* const* ctx_k, const void* const* ctx_v,
                             const ardit_block_weights* w, void* x0_out, void* ws,
                             size_t ws_bytes);
+
+/* ardit_chunk_generate with the linears in 8-bit integers, as in ardit_stack_fwd_int. */
+int ardit_chunk_generate_int(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                             int32_t n_layers, const int32_t* n_steps, const float* t_host,
+                             int32_t t_ld, const void* x_init, const void* noise,
+                             const ardit_kv_paged* kv, const ardit_time_weights* tw,
+                             const void* const* ctx_k, const void* const* ctx_v,
+                             const ardit_block_weights* w, const ardit_block_weights_int* w8,
+                             void* x0_out, void* ws, size_t ws_bytes);
 
 /* Kernel timing.  ardit_timing_enable(mask) turns on HIP events recorded on
  * the launch stream around each launch of the kinds in mask: bit 0 (1) the

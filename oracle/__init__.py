@@ -22,3 +22,4 @@ from . import sparse_ref  # noqa: F401
 from . import fp8_ref  # noqa: F401
 from . import chunk_ref  # noqa: F401
 from . import control_ref  # noqa: F401
+from . import int_ref  # noqa: F401

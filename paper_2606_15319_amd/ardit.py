@@ -78,6 +78,33 @@ class ardit_block_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _BLOCK_FIELDS]
 
 
+_INT_MATRICES = ("w_qkv", "w_o", "w_cq", "w_co", "w_1", "w_2")
+_INT_SCALES = ("s_qkv", "s_o", "s_cq", "s_co", "s_1", "s_2")
+
+
+class ardit_block_weights_int(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in _INT_MATRICES + _INT_SCALES]
+
+
+class ardit_norm_desc(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_type", C.c_int32), ("ldx", C.c_int64),
+                ("delta", C.c_void_p), ("delta_type", C.c_int32), ("ldd", C.c_int64),
+                ("h", C.c_void_p), ("ldh", C.c_int64), ("gain", C.c_void_p),
+                ("mod", C.c_void_p), ("mod_table", C.c_void_p), ("shift_row", C.c_int32),
+                ("scale_row", C.c_int32), ("gate_row", C.c_int32),
+                ("rows_per_stream", C.c_int64), ("eps", C.c_double)]
+
+
+class ardit_linear_desc(C.Structure):
+    _fields_ = [("m", C.c_int32), ("n", C.c_int32), ("k", C.c_int32),
+                ("x_codes", C.c_void_p), ("ldx", C.c_int64), ("x_scales", C.c_void_p),
+                ("w_codes", C.c_void_p), ("ldw", C.c_int64), ("w_scales", C.c_void_p),
+                ("bias", C.c_void_p), ("act", C.c_int32),
+                ("res", C.c_void_p), ("res_type", C.c_int32), ("ldr", C.c_int64),
+                ("mod", C.c_void_p), ("mod_table", C.c_void_p), ("gate_row", C.c_int32),
+                ("rows_per_stream", C.c_int64)]
+
+
 class ardit_time_weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in _TIME_FIELDS]
 
@@ -96,7 +123,7 @@ class ardit_stream_decision(C.Structure):
                 ("queue_pos", C.c_int32), ("credit_ms", C.c_double)]
 
 
-_vp, _i32, _sz = C.c_void_p, C.c_int32, C.c_size_t
+_vp, _i32, _i64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 _P = C.POINTER
 _SIGS = {
     "ardit_status_str": (C.c_char_p, [C.c_int]),
@@ -114,6 +141,10 @@ _SIGS = {
     "ardit_attn_fwd_noalloc": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp,
                                          _P(ardit_kv_paged), _vp]),
     "ardit_mx_quantize": (C.c_int, [_vp, _vp, C.c_int64, _i32, _i32, _vp, _vp]),
+    "ardit_int_quantize": (C.c_int, [_vp, _vp, _i32, _i64, _i32, _i64, _vp, _i64, _vp]),
+    "ardit_int_dequantize": (C.c_int, [_vp, _vp, _i64, _i32, _i64, _vp, _vp, _i32, _i64]),
+    "ardit_int_norm": (C.c_int, [_vp, _i64, _i32, _P(ardit_norm_desc), _vp, _i64, _vp]),
+    "ardit_int_linear": (C.c_int, [_vp, _P(ardit_linear_desc), _vp, _i32, _i64]),
     "ardit_kv_mx_bytes": (C.c_int, [_P(ardit_dims), _i32, _i32, _P(_sz), _P(_sz)]),
     "ardit_kv_append_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _vp, _vp, _vp,
                                      _P(ardit_kv_mx), _vp]),
@@ -134,6 +165,10 @@ _SIGS = {
     "ardit_stack_fwd_mx": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _vp,
                                      _P(ardit_kv_mx), _vp, _P(_vp), _P(_vp),
                                      _P(ardit_block_weights), _vp, _vp, _sz]),
+    "ardit_stack_fwd_int": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _vp,
+                                      _P(ardit_kv_paged), _vp, _P(_vp), _P(_vp),
+                                      _P(ardit_block_weights), _P(ardit_block_weights_int), _vp,
+                                      _vp, _sz]),
     "ardit_window_pages": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _P(_i32), _i32, _P(_i32)]),
     "ardit_chunk_generate": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _P(_i32),
                                        _P(C.c_float), _i32, _vp, _vp, _P(ardit_kv_paged),
@@ -143,6 +178,11 @@ _SIGS = {
                                           _P(C.c_float), _i32, _vp, _vp, _P(ardit_kv_mx),
                                           _P(ardit_time_weights), _P(_vp), _P(_vp),
                                           _P(ardit_block_weights), _vp, _vp, _sz]),
+    "ardit_chunk_generate_int": (C.c_int, [_vp, _P(ardit_dims), _P(ardit_batch), _i32, _P(_i32),
+                                           _P(C.c_float), _i32, _vp, _vp, _P(ardit_kv_paged),
+                                           _P(ardit_time_weights), _P(_vp), _P(_vp),
+                                           _P(ardit_block_weights), _P(ardit_block_weights_int),
+                                           _vp, _vp, _sz]),
     "ardit_pareto_frontier": (C.c_int, [_i32, _P(ardit_fidelity), _P(_i32), _P(_i32),
                                         _P(C.c_double)]),
     "ardit_bmpr_select": (C.c_int, [_i32, _P(ardit_fidelity), _i32, _P(_i32), C.c_double,
@@ -268,6 +308,33 @@ def block_weights(w: dict) -> ardit_block_weights:
     return ardit_block_weights(*[_ptr(w.get(n)) for n in _BLOCK_FIELDS])
 
 
+def block_weights_int(w: dict) -> ardit_block_weights_int:
+    """From codes w_qkv .. w_2 ([out][in] int8) and scales s_qkv .. s_2 (fp32 per row)."""
+    return ardit_block_weights_int(*[_ptr(w.get(n)) for n in _INT_MATRICES + _INT_SCALES])
+
+
+BF16, F32 = 0, 1
+ACT_NONE, ACT_GELU = 0, 1
+
+
+def norm_desc(x, x_type, ldx, delta=None, delta_type=BF16, ldd=0, h=None, ldh=0, gain=None, mod=None,
+              mod_table=None, rows_per_stream=1, shift_row=-1, scale_row=-1, gate_row=-1,
+              eps=1e-6) -> ardit_norm_desc:
+    return ardit_norm_desc(_ptr(x), int(x_type), int(ldx), _ptr(delta), int(delta_type), int(ldd),
+                           _ptr(h), int(ldh), _ptr(gain), _ptr(mod), _ptr(mod_table),
+                           int(shift_row), int(scale_row), int(gate_row), int(rows_per_stream),
+                           float(eps))
+
+
+def linear_desc(m, n, k, x_codes, ldx, x_scales, w_codes, ldw, w_scales, bias=None, act=ACT_NONE,
+                res=None, res_type=BF16, ldr=0, mod=None, mod_table=None, gate_row=-1,
+                rows_per_stream=1) -> ardit_linear_desc:
+    return ardit_linear_desc(int(m), int(n), int(k), _ptr(x_codes), int(ldx), _ptr(x_scales),
+                             _ptr(w_codes), int(ldw), _ptr(w_scales), _ptr(bias), int(act),
+                             _ptr(res), int(res_type), int(ldr), _ptr(mod), _ptr(mod_table),
+                             int(gate_row), int(rows_per_stream))
+
+
 def time_weights(w: dict) -> ardit_time_weights:
     return ardit_time_weights(*[_ptr(w[n]) for n in _TIME_FIELDS])
 
@@ -315,6 +382,29 @@ QUANT_BF16, QUANT_FP8 = 0, 1
 def ardit_mx_quantize(stream, x, rows, cols, ld, codes, scales):
     _check(_lib.ardit_mx_quantize(_stream(stream), _ptr(x), int(rows), int(cols), int(ld),
                                   _ptr(codes), _ptr(scales)), "ardit_mx_quantize")
+
+
+def ardit_int_quantize(stream, x, x_type, rows, cols, ldx, codes, ldc, scales):
+    """Rows of x to int8 codes and a scale each (BF16 or F32)."""
+    _check(_lib.ardit_int_quantize(_stream(stream), _ptr(x), int(x_type), int(rows), int(cols),
+                                   int(ldx), _ptr(codes), int(ldc), _ptr(scales)),
+           "ardit_int_quantize")
+
+
+def ardit_int_dequantize(stream, codes, rows, cols, ldc, scales, y, y_type, ldy):
+    _check(_lib.ardit_int_dequantize(_stream(stream), _ptr(codes), int(rows), int(cols), int(ldc),
+                                     _ptr(scales), _ptr(y), int(y_type), int(ldy)),
+           "ardit_int_dequantize")
+
+
+def ardit_int_norm(stream, rows, dim, norm: ardit_norm_desc, codes, ldc, scales):
+    _check(_lib.ardit_int_norm(_stream(stream), int(rows), int(dim), C.byref(norm), _ptr(codes),
+                               int(ldc), _ptr(scales)), "ardit_int_norm")
+
+
+def ardit_int_linear(stream, linear: ardit_linear_desc, y, y_type, ldy):
+    _check(_lib.ardit_int_linear(_stream(stream), C.byref(linear), _ptr(y), int(y_type), int(ldy)),
+           "ardit_int_linear")
 
 
 KV_E4M3, KV_E2M1 = 1, 2
@@ -369,15 +459,23 @@ def ardit_block_fwd_varlen(stream, dims, batch: Batch, x, kv: ardit_kv_paged, mo
            "ardit_block_fwd_varlen")
 
 
+def _weight_arrays(ws_list, w8_list, n):
+    """Per-layer weight arguments: one array, or with w8_list two."""
+    arrays = [(ardit_block_weights * n)(*ws_list)]
+    if w8_list is not None:
+        arrays.append((ardit_block_weights_int * n)(*w8_list))
+    return arrays
+
+
 def _stack(name, kv_type, stream, dims, batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, out, ws,
-           ws_bytes):
+           ws_bytes, w8_list=None):
     L = len(kvs)
     kv_arr = (kv_type * L)(*kvs)
-    w_arr = (ardit_block_weights * L)(*ws_list)
+    w_arr = _weight_arrays(ws_list, w8_list, L)
     ck = (C.c_void_p * L)(*[_ptr(t) for t in ctx_ks])
     cv = (C.c_void_p * L)(*[_ptr(t) for t in ctx_vs])
     _check(getattr(_lib, name)(_stream(stream), C.byref(dims), C.byref(batch.struct), L, _ptr(x),
-                               kv_arr, _ptr(mod), ck, cv, w_arr, _ptr(out), _ptr(ws),
+                               kv_arr, _ptr(mod), ck, cv, *w_arr, _ptr(out), _ptr(ws),
                                int(ws_bytes)), name)
 
 
@@ -394,6 +492,13 @@ def ardit_stack_fwd_mx(stream, dims, batch: Batch, x, kvs, mod, ctx_ks, ctx_vs, 
            ws_list, out, ws, ws_bytes)
 
 
+def ardit_stack_fwd_int(stream, dims, batch: Batch, x, kvs, mod, ctx_ks, ctx_vs, ws_list, w8_list, out,
+                        ws, ws_bytes):
+    """w8_list: ardit_block_weights_int per layer."""
+    _stack("ardit_stack_fwd_int", ardit_kv_paged, stream, dims, batch, x, kvs, mod, ctx_ks, ctx_vs,
+           ws_list, out, ws, ws_bytes, w8_list)
+
+
 def ardit_window_pages(chunk, sink, window, frames_per_chunk, page_base=0, max_frames=None):
     """Returns (table entries of the held chunks then the chunk, cached frames)."""
     if max_frames is None:
@@ -408,7 +513,7 @@ def ardit_window_pages(chunk, sink, window, frames_per_chunk, page_base=0, max_f
 
 
 def _chunk(name, kv_type, stream, dims, batch, n_steps, timesteps, x_init, noise, kvs, tw, ctx_ks,
-           ctx_vs, ws_list, x0_out, ws, ws_bytes):
+           ctx_vs, ws_list, x0_out, ws, ws_bytes, w8_list=None):
     L = len(kvs)
     B = len(n_steps)
     t_ld = max(1, max(int(s) for s in n_steps))
@@ -418,11 +523,11 @@ def _chunk(name, kv_type, stream, dims, batch, n_steps, timesteps, x_init, noise
             t[b * t_ld + i] = float(v)
     ns = (C.c_int32 * B)(*[int(v) for v in n_steps])
     kv_arr = (kv_type * L)(*kvs)
-    w_arr = (ardit_block_weights * L)(*ws_list)
+    w_arr = _weight_arrays(ws_list, w8_list, L)
     ck = (C.c_void_p * L)(*[_ptr(x) for x in ctx_ks])
     cv = (C.c_void_p * L)(*[_ptr(x) for x in ctx_vs])
     _check(getattr(_lib, name)(_stream(stream), C.byref(dims), C.byref(batch.struct), L, ns, t,
-                               t_ld, _ptr(x_init), _ptr(noise), kv_arr, C.byref(tw), ck, cv, w_arr,
+                               t_ld, _ptr(x_init), _ptr(noise), kv_arr, C.byref(tw), ck, cv, *w_arr,
                                _ptr(x0_out), _ptr(ws), int(ws_bytes)), name)
 
 
@@ -438,6 +543,14 @@ def ardit_chunk_generate_mx(stream, dims, batch: Batch, n_steps, timesteps, x_in
     """kvs: ardit_kv_mx per layer; the rest as for ardit_chunk_generate."""
     _chunk("ardit_chunk_generate_mx", ardit_kv_mx, stream, dims, batch, n_steps, timesteps, x_init,
            noise, kvs, tw, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes)
+
+
+def ardit_chunk_generate_int(stream, dims, batch: Batch, n_steps, timesteps, x_init, noise, kvs,
+                             tw: ardit_time_weights, ctx_ks, ctx_vs, ws_list, w8_list, x0_out, ws,
+                             ws_bytes):
+    """w8_list: ardit_block_weights_int per layer; the rest as for ardit_chunk_generate."""
+    _chunk("ardit_chunk_generate_int", ardit_kv_paged, stream, dims, batch, n_steps, timesteps, x_init,
+           noise, kvs, tw, ctx_ks, ctx_vs, ws_list, x0_out, ws, ws_bytes, w8_list)
 
 
 TIME_ATTENTION, TIME_GEMM, TIME_ELEMENTWISE = 0, 1, 2

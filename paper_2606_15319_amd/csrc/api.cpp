@@ -359,6 +359,48 @@ int check_ptr(const void* p, const char* name) {
   return ARDIT_OK;
 }
 
+// ---- 8-bit integers
+constexpr int64_t kIntMaxRows = 1 << 22;
+constexpr int32_t kIntMaxCols = 65536;    // (32-bit sums: 65536 * 128^2 = 2^30)
+constexpr int32_t kIntMaxNorm = 8192;
+constexpr int32_t kIntMaxOut = 1 << 20;
+constexpr int64_t kIntMaxStride = 1 << 20;         // bytes, of codes (tiles are addressed in 32 bits)
+constexpr int64_t kIntMaxElems = int64_t(1) << 32; // elements, of other rows
+
+int check_rows(int64_t rows, int64_t cols, int32_t most) {
+  if (rows < 0) return fail(ARDIT_ESHAPE, "%lld rows", static_cast<long long>(rows));
+  if (rows > kIntMaxRows) return fail(ARDIT_ECAPACITY, "%lld rows above 2^22", static_cast<long long>(rows));
+  if (cols < 1 || cols > most)
+    return fail(ARDIT_ESHAPE, "rows of %lld, not in [1, %d]", static_cast<long long>(cols), most);
+  return ARDIT_OK;
+}
+
+int check_elems(const void* p, int size, const char* name) {
+  if (!p) return fail(ARDIT_EINVAL, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % size != 0)
+    return fail(ARDIT_EINVAL, "%s must be %d-byte aligned", name, size);
+  return ARDIT_OK;
+}
+
+// a tensor of rows of `cols` elements (`none`: there are no rows, so no memory either)
+int check_tensor(const void* p, int32_t type, int64_t ld, int64_t cols, bool none, const char* name) {
+  if (type != ARDIT_BF16 && type != ARDIT_F32)
+    return fail(ARDIT_EINVAL, "%s: %d is not an element type", name, type);
+  if (ld < cols || ld > kIntMaxElems)
+    return fail(ARDIT_ESHAPE, "%s: row stride %lld not in [%lld, 2^32]", name, static_cast<long long>(ld),
+                static_cast<long long>(cols));
+  return none ? ARDIT_OK : check_elems(p, type == ARDIT_F32 ? 4 : 2, name);
+}
+
+int check_codes(const void* p, int64_t ld, const float* scales, int64_t cols, bool none, const char* name) {
+  if (ld < cols || ld % 16 != 0 || ld > kIntMaxStride)
+    return fail(ARDIT_ESHAPE, "%s: row stride %lld is not a multiple of 16 in [%lld, 2^20]", name,
+                static_cast<long long>(ld), static_cast<long long>(cols));
+  if (none) return ARDIT_OK;
+  ARDIT_TRY(check_elems(p, 16, name));
+  return check_elems(scales, 4, "scales");
+}
+
 int check_block_weights(const ardit_block_weights* w, bool ctx) {
   if (!w) return fail(ARDIT_EINVAL, "weights is NULL");
   if (ctx) {
@@ -374,6 +416,36 @@ int check_block_weights(const ardit_block_weights* w, bool ctx) {
                      w->mod_table};
   const char* n[] = {"w_qkv", "b_qkv", "g_q", "g_k", "w_o", "b_o", "g_n3", "w_cq", "b_cq",
                      "g_cq", "w_co", "b_co", "w_1", "b_1", "w_2", "b_2", "mod_table"};
+  for (size_t i = 0; i < sizeof(p) / sizeof(p[0]); ++i) ARDIT_TRY(check_ptr(p[i], n[i]));
+  return ARDIT_OK;
+}
+
+// One layer's weights with its matrices in 8-bit integers, and the arrays of all layers.
+struct IntLayer {
+  const ardit_block_weights* w;
+  const ardit_block_weights_int* w8;
+};
+struct IntWeights {
+  const ardit_block_weights* w;
+  const ardit_block_weights_int* w8;
+};
+const ardit_block_weights* layer_of(const ardit_block_weights* w, int l) { return w + l; }
+IntLayer layer_of(const IntWeights& w, int l) { return IntLayer{w.w + l, w.w8 + l}; }
+bool missing(const ardit_block_weights* w) { return !w; }
+bool missing(const IntWeights& w) { return !w.w || !w.w8; }
+
+int check_layer(const ardit_dims*, const ardit_block_weights* w) { return check_block_weights(w, false); }
+int check_layer(const ardit_dims* d, const IntLayer& l) {
+  if (d->ffn_dim > 15 * d->dim)   // (the codes of the FFN's rows share the workspace of earlier steps)
+    return fail(ARDIT_EUNSUPPORTED, "8-bit linears need ffn_dim %d <= 15 dim %d", d->ffn_dim, d->dim);
+  const ardit_block_weights* w = l.w;
+  const void* p[] = {w->b_qkv, w->g_q, w->g_k, w->b_o, w->g_n3, w->b_cq, w->g_cq, w->b_co, w->b_1,
+                     w->b_2, w->mod_table, l.w8->w_qkv, l.w8->w_o, l.w8->w_cq, l.w8->w_co,
+                     l.w8->w_1, l.w8->w_2, l.w8->s_qkv, l.w8->s_o, l.w8->s_cq, l.w8->s_co,
+                     l.w8->s_1, l.w8->s_2};
+  const char* n[] = {"b_qkv", "g_q", "g_k", "b_o", "g_n3", "b_cq", "g_cq", "b_co", "b_1",
+                     "b_2", "mod_table", "codes w_qkv", "codes w_o", "codes w_cq", "codes w_co",
+                     "codes w_1", "codes w_2", "s_qkv", "s_o", "s_cq", "s_co", "s_1", "s_2"};
   for (size_t i = 0; i < sizeof(p) / sizeof(p[0]); ++i) ARDIT_TRY(check_ptr(p[i], n[i]));
   return ARDIT_OK;
 }
@@ -876,6 +948,108 @@ int block_chain(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const
   return ARDIT_OK;
 }
 
+// The block chain with its linears over 8-bit integer codes.  The codes of a product's input lie
+// where h does in the bf16 chain, scales behind them; those of the FFN's rows go on over qkv, q, o
+// and x1, which are done with by then.
+template <typename KV>
+int block_chain(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* xin,
+                const KV* kv, const float* mod, const void* ctx_k, const void* ctx_v,
+                const IntLayer& layer, void* out, void* ws, const Ws& L, bool kv_only = false) {
+  const ardit_block_weights* w = layer.w;
+  const ardit_block_weights_int* w8 = layer.w8;
+  const int N = static_cast<int>(sum_q(b));
+  const int D = d->dim, F = d->ffn_dim, hd = d->head_dim;
+  const int Lq = chunk_tokens(d);
+  bf16_t* qkv = at<bf16_t>(ws, L.qkv);
+  bf16_t* q = at<bf16_t>(ws, L.q);
+  bf16_t* o = at<bf16_t>(ws, L.o);
+  float* x1 = at<float>(ws, L.x1);
+  float* x2 = at<float>(ws, L.x2);
+  bf16_t* u = at<bf16_t>(ws, L.u);
+  int8_t* codes = at<int8_t>(ws, L.h);
+  float* scales = at<float>(ws, L.h + up(static_cast<size_t>(N) * D));
+  float* scales_u = at<float>(ws, L.h + up(static_cast<size_t>(N) * F));
+
+  auto norm = [&](const void* x, bool f32, const void* gain, int shift_row, int scale_row) {
+    IntNormArgs a = {};
+    a.x = x;
+    a.x_f32 = f32;
+    a.ldx = D;
+    a.gain = static_cast<const bf16_t*>(gain);
+    a.mod = mod;
+    a.table = w->mod_table;
+    a.a_row = scale_row;
+    a.shift_row = shift_row;
+    a.gate_row = -1;
+    a.rows_per_stream = gain ? N : Lq;
+    a.rows = N;
+    a.D = D;
+    a.eps = d->eps;
+    a.codes = codes;
+    a.ldc = D;
+    a.scales = scales;
+    return launch_int_norm(st, a);
+  };
+  auto quantize = [&](const bf16_t* x, int cols, float* s) {
+    return launch_int_quantize(st, IntRows{x, false, N, cols, cols}, codes, cols, s);
+  };
+  // y = epilogue(codes W^T) of K columns; a residual of type res_f32 where res is given, gated
+  // by row gate_row of the modulation where that is not negative
+  auto linear = [&](int K, const float* s, const void* wc, const float* wsc, const void* bias, int n, int epi,
+                    void* y, bool y_f32, const void* res = nullptr, bool res_f32 = false, int gate_row = -1) {
+    IntGemmArgs a = {};
+    a.x = codes;
+    a.ldx = K;
+    a.sx = s;
+    a.w = static_cast<const int8_t*>(wc);
+    a.ldw = K;
+    a.sw = wsc;
+    a.M = N;
+    a.N = n;
+    a.K = K;
+    a.bias = static_cast<const bf16_t*>(bias);
+    a.res = res;
+    a.res_f32 = res_f32;
+    a.ldr = n;
+    a.mod = mod;
+    a.table = w->mod_table;
+    a.gate_row = gate_row;
+    a.rows_per_stream = make_fastdiv(Lq);
+    a.y = y;
+    a.y_f32 = y_f32;
+    a.ldy = n;
+    return launch_int_gemm(st, epi, a);
+  };
+
+  ARDIT_TIMED(kTimeElem, norm(xin, false, nullptr, 0, 1), "adaln_norm codes");
+  ARDIT_TIMED(kTimeGemm, linear(D, scales, w8->w_qkv, w8->s_qkv, w->b_qkv, 3 * D, kEpiBias, qkv, false),
+              "qkv int gemm");
+  ARDIT_TRY(block_append(st, d, b, qkv, w, kv, q));
+  if (kv_only) return ARDIT_OK;
+  ARDIT_TRY(block_attention(st, d, b, q, kv, o, ws, L));
+  ARDIT_TIMED(kTimeElem, quantize(o, D, scales), "attention codes");
+  ARDIT_TIMED(kTimeGemm, linear(D, scales, w8->w_o, w8->s_o, w->b_o, D, kEpiBiasGateRes, x1, true, xin, false, 2),
+              "o int gemm");
+  ARDIT_TIMED(kTimeElem, norm(x1, true, w->g_n3, -1, -1), "cross pre-norm codes");
+  ARDIT_TIMED(kTimeGemm, linear(D, scales, w8->w_cq, w8->s_cq, w->b_cq, D, kEpiBias, q, false), "cq int gemm");
+  ARDIT_TIMED(kTimeElem,
+              launch_rms_gain(st, q, false, q, N, D, static_cast<const bf16_t*>(w->g_cq), d->eps),
+              "cross q-norm");
+  const AttnArgs ca = cross_attn_args(d, b, q, ctx_k, ctx_v, o, at<float>(ws, L.attn));
+  ARDIT_HIP(launch_attention(st, ca, hd, false), "cross-attention");
+  ARDIT_TIMED(kTimeElem, quantize(o, D, scales), "cross-attention codes");
+  ARDIT_TIMED(kTimeGemm, linear(D, scales, w8->w_co, w8->s_co, w->b_co, D, kEpiBiasRes, x2, true, x1, true),
+              "co int gemm");
+  ARDIT_TIMED(kTimeElem, norm(x2, true, nullptr, 3, 4), "adaln_norm 2 codes");
+  ARDIT_TIMED(kTimeGemm, linear(D, scales, w8->w_1, w8->s_1, w->b_1, F, kEpiBiasGelu, u, false),
+              "ffn up int gemm");
+  ARDIT_TIMED(kTimeElem, quantize(u, F, scales_u), "ffn codes");
+  ARDIT_TIMED(kTimeGemm,
+              linear(F, scales_u, w8->w_2, w8->s_2, w->b_2, D, kEpiBiasGateRes, out, false, x2, true, 5),
+              "ffn down int gemm");
+  return ARDIT_OK;
+}
+
 int check_time_weights(const ardit_time_weights* tw) {
   if (!tw) return fail(ARDIT_EINVAL, "time weights NULL");
   const void* p[] = {tw->w_t1, tw->b_t1, tw->w_t2, tw->b_t2, tw->w_m, tw->b_m};
@@ -908,10 +1082,10 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
   return na && nb && x < y + nb && y < x + na;
 }
 
-template <typename KV>
+template <typename KV, typename W>
 int check_block_args(hipStream_t st, const ardit_dims* d, const ardit_batch* b, const void* x,
                      const KV* kv, const float* mod, const void* ctx_k,
-                     const void* ctx_v, const ardit_block_weights* w, const void* out) {
+                     const void* ctx_v, const W& w, const void* out) {
   ARDIT_TRY(check_dims(d));
   ARDIT_TRY(check_batch(d, b, kUseQ | kUseCache | kUsePos | kUseCtx | kChunkQ));
   ARDIT_TRY(check_kv(d, b, kv));
@@ -921,20 +1095,20 @@ int check_block_args(hipStream_t st, const ardit_dims* d, const ardit_batch* b, 
   ARDIT_TRY(check_ptr(mod, "mod"));
   ARDIT_TRY(check_ptr(ctx_k, "ctx_k"));
   ARDIT_TRY(check_ptr(ctx_v, "ctx_v"));
-  ARDIT_TRY(check_block_weights(w, false));
+  ARDIT_TRY(check_layer(d, w));
   return check_pages(st, d, b, kv, true);
 }
 
-// n_layers blocks over either kind of cache
-template <typename KV>
+// n_layers blocks over either kind of cache, with either kind of weights
+template <typename KV, typename W>
 int stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch, int32_t n_layers,
               const void* x, const KV* kv, const float* mod, const void* const* ctx_k,
-              const void* const* ctx_v, const ardit_block_weights* w, void* out, void* ws,
-              size_t ws_bytes) {
+              const void* const* ctx_v, const W& w, void* out, void* ws, size_t ws_bytes) {
   if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
-  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
+  if (!kv || !ctx_k || !ctx_v || missing(w)) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
   for (int l = 0; l < n_layers; ++l)
-    ARDIT_TRY(check_block_args(stream, dims, batch, x, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l], out));
+    ARDIT_TRY(check_block_args(stream, dims, batch, x, &kv[l], mod, ctx_k[l], ctx_v[l],
+                               layer_of(w, l), out));
   if (x == out) return fail(ARDIT_EINVAL, "stack input and output must differ");
   Ws L;
   ARDIT_TRY(check_ws(dims, batch, ws, ws_bytes, &L));
@@ -942,22 +1116,21 @@ int stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batch* bat
   // layer reads its input only before it writes its output)
   for (int l = 0; l < n_layers; ++l)
     ARDIT_TRY(block_chain(stream, dims, batch, l == 0 ? x : out, &kv[l], mod, ctx_k[l], ctx_v[l],
-                          &w[l], out, ws, L));
+                          layer_of(w, l), out, ws, L));
   return ARDIT_OK;
 }
 
-// a chunk's denoising and commit passes over either kind of cache
-template <typename KV>
+// a chunk's denoising and commit passes over either kind of cache, with either kind of weights
+template <typename KV, typename W>
 int chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
                    int32_t n_layers, const int32_t* n_steps, const float* t_host, int32_t t_ld,
                    const void* x_init, const void* noise, const KV* kv,
                    const ardit_time_weights* tw, const void* const* ctx_k,
-                   const void* const* ctx_v, const ardit_block_weights* w, void* x0_out, void* ws,
-                   size_t ws_bytes) {
+                   const void* const* ctx_v, const W& w, void* x0_out, void* ws, size_t ws_bytes) {
   ARDIT_TRY(check_dims(dims));
   ARDIT_TRY(check_batch(dims, batch, kUseQ | kUseCache | kUsePos | kUseCtx | kChunkQ));
   if (n_layers < 1) return fail(ARDIT_EINVAL, "n_layers %d must be >= 1", n_layers);
-  if (!kv || !ctx_k || !ctx_v || !w) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
+  if (!kv || !ctx_k || !ctx_v || missing(w)) return fail(ARDIT_EINVAL, "per-layer arrays must be non-NULL");
   if (!n_steps || !t_host) return fail(ARDIT_EINVAL, "n_steps and t_host must be non-NULL");
   const int B = batch->n_streams;
   const int S0 = n_steps[0];
@@ -985,8 +1158,8 @@ int chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit_batch
   float* mod = at<float>(ws, L.gmod);
   bf16_t* vel = at<bf16_t>(ws, L.gv);
   for (int l = 0; l < n_layers; ++l)
-    ARDIT_TRY(check_block_args(stream, dims, batch, x_init, &kv[l], mod, ctx_k[l], ctx_v[l], &w[l],
-                               vel));
+    ARDIT_TRY(check_block_args(stream, dims, batch, x_init, &kv[l], mod, ctx_k[l], ctx_v[l],
+                               layer_of(w, l), vel));
   const int64_t N = sum_q(batch);
   const int D = dims->dim;
   const size_t xbytes = 2 * static_cast<size_t>(N) * D;
@@ -1021,7 +1194,7 @@ int chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit_batch
     const bool commit_only = denoise == 0;
     for (int l = 0; l < n_layers; ++l)
       ARDIT_TRY(block_chain(stream, dims, &sb, l == 0 ? xin : vel, &kv[l], mod, ctx_k[l],
-                            ctx_v[l], &w[l], vel, ws, L, commit_only && l == n_layers - 1));
+                            ctx_v[l], layer_of(w, l), vel, ws, L, commit_only && l == n_layers - 1));
     if (denoise > 0) {
       sa.rows = denoise * Lq;
       sa.rows_per_stream = Lq;
@@ -1281,6 +1454,156 @@ int ardit_mx_quantize(hipStream_t stream, const void* x, int64_t rows, int32_t c
   return host_failure();
 }
 
+int ardit_int_quantize(hipStream_t stream, const void* x, int32_t x_type, int64_t rows, int32_t cols,
+                       int64_t ldx, void* codes, int64_t ldc, float* scales) try {
+  ARDIT_TRY(check_rows(rows, cols, kIntMaxCols));
+  ARDIT_TRY(check_tensor(x, x_type, ldx, cols, rows == 0, "x"));
+  ARDIT_TRY(check_codes(codes, ldc, scales, cols, rows == 0, "codes"));
+  if (rows == 0) return ARDIT_OK;
+  const IntRows r{x, x_type == ARDIT_F32, static_cast<int>(rows), cols, ldx};
+  ARDIT_HIP(launch_int_quantize(stream, r, static_cast<int8_t*>(codes), ldc, scales),
+            "row quantisation launch");
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_int_dequantize(hipStream_t stream, const void* codes, int64_t rows, int32_t cols, int64_t ldc,
+                         const float* scales, void* y, int32_t y_type, int64_t ldy) try {
+  ARDIT_TRY(check_rows(rows, cols, kIntMaxCols));
+  ARDIT_TRY(check_codes(codes, ldc, scales, cols, rows == 0, "codes"));
+  ARDIT_TRY(check_tensor(y, y_type, ldy, cols, rows == 0, "y"));
+  if (rows == 0) return ARDIT_OK;
+  ARDIT_HIP(launch_int_dequantize(stream, static_cast<const int8_t*>(codes), ldc, scales, y,
+                                  y_type == ARDIT_F32, ldy, static_cast<int>(rows), cols),
+            "read-back launch");
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_int_norm(hipStream_t stream, int64_t rows, int32_t dim, const ardit_norm_desc* norm,
+                   void* codes, int64_t ldc, float* scales) try {
+  if (!norm) return fail(ARDIT_EINVAL, "norm is NULL");
+  ARDIT_TRY(check_rows(rows, dim, kIntMaxNorm));
+  const bool none = rows == 0;
+  ARDIT_TRY(check_tensor(norm->x, norm->x_type, norm->ldx, dim, none, "x"));
+  if (norm->delta)
+    ARDIT_TRY(check_tensor(norm->delta, norm->delta_type, norm->ldd, dim, none, "delta"));
+  if (norm->h) {
+    ARDIT_TRY(check_tensor(norm->h, ARDIT_F32, norm->ldh, dim, none, "h"));
+    if (norm->h == norm->x && (norm->x_type != ARDIT_F32 || norm->ldh != norm->ldx))
+      return fail(ARDIT_EINVAL, "h over x needs fp32 and the same stride");
+    if (norm->h == norm->delta && (norm->delta_type != ARDIT_F32 || norm->ldh != norm->ldd))
+      return fail(ARDIT_EINVAL, "h over delta needs fp32 and the same stride");
+  }
+  const int32_t named[] = {norm->shift_row, norm->scale_row, norm->gate_row};
+  bool any = false;
+  for (int32_t r : named) {
+    if (r < -1 || r > 5) return fail(ARDIT_EINVAL, "modulation row %d not in [-1, 5]", r);
+    any |= r >= 0;
+  }
+  if (any) {
+    if (norm->rows_per_stream < 1) return fail(ARDIT_EINVAL, "rows_per_stream must be >= 1");
+    if (!none) ARDIT_TRY(check_elems(norm->mod, 4, "mod"));
+    if (norm->mod_table) ARDIT_TRY(check_elems(norm->mod_table, 4, "mod_table"));
+  }
+  if (norm->gate_row >= 0 && !norm->delta) return fail(ARDIT_EINVAL, "a gate needs delta");
+  if (norm->gain) {
+    ARDIT_TRY(check_elems(norm->gain, 2, "gain"));
+    if (norm->shift_row >= 0 || norm->scale_row >= 0)
+      return fail(ARDIT_EINVAL, "gain together with shift or scale");
+  }
+  if (!(norm->eps > 0.0) || !(norm->eps <= 1e300)) return fail(ARDIT_EINVAL, "eps must be positive");
+  ARDIT_TRY(check_codes(codes, ldc, scales, dim, none, "codes"));
+  if (none) return ARDIT_OK;
+  IntNormArgs a = {};
+  a.x = norm->x;
+  a.x_f32 = norm->x_type == ARDIT_F32;
+  a.ldx = norm->ldx;
+  a.dk = !norm->delta ? 0 : norm->delta_type == ARDIT_F32 ? 2 : 1;
+  a.delta = norm->delta;
+  a.ldd = norm->ldd;
+  a.h = norm->h;
+  a.ldh = norm->ldh;
+  a.gain = static_cast<const bf16_t*>(norm->gain);
+  a.mod = norm->mod;
+  a.table = norm->mod_table;
+  a.a_row = norm->scale_row;
+  a.shift_row = norm->shift_row;
+  a.gate_row = norm->gate_row;
+  a.rows_per_stream = any ? norm->rows_per_stream : rows;
+  a.rows = static_cast<int>(rows);
+  a.D = dim;
+  a.eps = norm->eps;
+  a.codes = static_cast<int8_t*>(codes);
+  a.ldc = ldc;
+  a.scales = scales;
+  ARDIT_HIP(launch_int_norm(stream, a), "norm launch");
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_int_linear(hipStream_t stream, const ardit_linear_desc* l, void* y, int32_t y_type,
+                     int64_t ldy) try {
+  if (!l) return fail(ARDIT_EINVAL, "linear is NULL");
+  ARDIT_TRY(check_rows(l->m, l->k, kIntMaxCols));
+  if (l->n < 1 || l->n > kIntMaxOut)
+    return fail(ARDIT_ESHAPE, "n %d not in [1, %d]", l->n, kIntMaxOut);
+  const bool none = l->m == 0;
+  ARDIT_TRY(check_codes(l->x_codes, l->ldx, l->x_scales, l->k, none, "x_codes"));
+  ARDIT_TRY(check_codes(l->w_codes, l->ldw, l->w_scales, l->k, none, "w_codes"));
+  ARDIT_TRY(check_tensor(y, y_type, ldy, l->n, none, "y"));
+  if (l->bias) ARDIT_TRY(check_elems(l->bias, 2, "bias"));
+  if (l->act != ARDIT_ACT_NONE && l->act != ARDIT_ACT_GELU)
+    return fail(ARDIT_EINVAL, "act %d is not an activation", l->act);
+  if (l->act == ARDIT_ACT_GELU && l->res) return fail(ARDIT_EUNSUPPORTED, "GELU with a residual");
+  if (l->act == ARDIT_ACT_GELU && y_type != ARDIT_BF16) return fail(ARDIT_EUNSUPPORTED, "GELU gives bf16");
+  if (l->gate_row < -1 || l->gate_row > 5)
+    return fail(ARDIT_EINVAL, "modulation row %d not in [-1, 5]", l->gate_row);
+  if (l->gate_row >= 0) {
+    if (!l->res) return fail(ARDIT_EINVAL, "a gate needs res");
+    if (l->rows_per_stream < 1) return fail(ARDIT_EINVAL, "rows_per_stream must be >= 1");
+    if (!none) ARDIT_TRY(check_elems(l->mod, 4, "mod"));
+    if (l->mod_table) ARDIT_TRY(check_elems(l->mod_table, 4, "mod_table"));
+  }
+  if (l->res) {
+    ARDIT_TRY(check_tensor(l->res, l->res_type, l->ldr, l->n, none, "res"));
+    if (l->res == y && (l->res_type != y_type || l->ldr != ldy))
+      return fail(ARDIT_EINVAL, "y over res needs the same type and stride");
+  }
+  if (none) return ARDIT_OK;
+  IntGemmArgs a = {};
+  a.x = static_cast<const int8_t*>(l->x_codes);
+  a.ldx = l->ldx;
+  a.sx = l->x_scales;
+  a.w = static_cast<const int8_t*>(l->w_codes);
+  a.ldw = l->ldw;
+  a.sw = l->w_scales;
+  a.M = l->m;
+  a.N = l->n;
+  a.K = l->k;
+  a.bias = static_cast<const bf16_t*>(l->bias);
+  a.res = l->res;
+  a.res_f32 = l->res && l->res_type == ARDIT_F32;
+  a.ldr = l->ldr;
+  a.mod = l->mod;
+  a.table = l->mod_table;
+  a.gate_row = l->gate_row;
+  a.rows_per_stream = make_fastdiv(
+      l->gate_row >= 0 ? static_cast<uint32_t>(l->rows_per_stream < l->m ? l->rows_per_stream : l->m) : 1);
+  a.y = y;
+  a.y_f32 = y_type == ARDIT_F32;
+  a.ldy = ldy;
+  const int epi = l->act == ARDIT_ACT_GELU ? kEpiBiasGelu
+                  : !l->res ? kEpiBias : l->gate_row >= 0 ? kEpiBiasGateRes : kEpiBiasRes;
+  ARDIT_HIP(launch_int_gemm(stream, epi, a), "integer linear launch");
+  return ARDIT_OK;
+} catch (...) {
+  return host_failure();
+}
+
 int ardit_kv_mx_bytes(const ardit_dims* dims, int32_t format, int32_t n_pages, size_t* code_bytes,
                       size_t* scale_bytes) try {
   ARDIT_TRY(check_dims(dims));
@@ -1431,6 +1754,17 @@ int ardit_stack_fwd(hipStream_t stream, const ardit_dims* dims, const ardit_batc
   return host_failure();
 }
 
+int ardit_stack_fwd_int(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                        int32_t n_layers, const void* x, const ardit_kv_paged* kv, const float* mod,
+                        const void* const* ctx_k, const void* const* ctx_v,
+                        const ardit_block_weights* w, const ardit_block_weights_int* w8, void* out,
+                        void* ws, size_t ws_bytes) try {
+  return stack_fwd(stream, dims, batch, n_layers, x, kv, mod, ctx_k, ctx_v, IntWeights{w, w8}, out, ws,
+                   ws_bytes);
+} catch (...) {
+  return host_failure();
+}
+
 int ardit_stack_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
                        int32_t n_layers, const void* x, const ardit_kv_mx* kv, const float* mod,
                        const void* const* ctx_k, const void* const* ctx_v,
@@ -1482,6 +1816,19 @@ int ardit_chunk_generate(hipStream_t stream, const ardit_dims* dims, const ardit
                          const ardit_block_weights* w, void* x0_out, void* ws, size_t ws_bytes) try {
   return chunk_generate(stream, dims, batch, n_layers, n_steps, t_host, t_ld, x_init, noise, kv, tw,
                         ctx_k, ctx_v, w, x0_out, ws, ws_bytes);
+} catch (...) {
+  return host_failure();
+}
+
+int ardit_chunk_generate_int(hipStream_t stream, const ardit_dims* dims, const ardit_batch* batch,
+                             int32_t n_layers, const int32_t* n_steps, const float* t_host,
+                             int32_t t_ld, const void* x_init, const void* noise,
+                             const ardit_kv_paged* kv, const ardit_time_weights* tw,
+                             const void* const* ctx_k, const void* const* ctx_v,
+                             const ardit_block_weights* w, const ardit_block_weights_int* w8,
+                             void* x0_out, void* ws, size_t ws_bytes) try {
+  return chunk_generate(stream, dims, batch, n_layers, n_steps, t_host, t_ld, x_init, noise, kv, tw,
+                        ctx_k, ctx_v, IntWeights{w, w8}, x0_out, ws, ws_bytes);
 } catch (...) {
   return host_failure();
 }

@@ -320,4 +320,65 @@ hipError_t launch_micro_read(hipStream_t st, const void* src, size_t bytes, uint
 // dst filled with a 32-bit value, bytes / 16 chunks of 16 bytes
 hipError_t launch_fill(hipStream_t st, void* dst, size_t bytes, uint32_t value);
 
+// ------------------------------------------------------------ 8-bit integers
+// Rows of bf16 or fp32 elements.
+struct IntRows {
+  const void* p;
+  bool f32;
+  int rows, cols;
+  int64_t ld;
+};
+
+// Rows to codes (int8, row stride ldc bytes, a multiple of 16) and fp32 scales.
+hipError_t launch_int_quantize(hipStream_t st, const IntRows& r, int8_t* codes, int64_t ldc, float* scales);
+// Codes to bf16 or fp32.
+hipError_t launch_int_dequantize(hipStream_t st, const int8_t* codes, int64_t ldc, const float* scales, void* y,
+                                 bool y_f32, int64_t ldy, int rows, int cols);
+
+struct IntNormArgs {
+  const void* x;
+  bool x_f32;
+  int dk;              // delta: 0 none, 1 bf16, 2 fp32
+  int64_t ldx;
+  const void* delta;
+  int64_t ldd;
+  float* h;            // or null
+  int64_t ldh;
+  const bf16_t* gain;  // or null
+  const float* mod;    // [streams][6][D]
+  const float* table;  // [6][D] or null
+  int a_row, shift_row, gate_row;   // rows of the modulation, -1: none
+  int64_t rows_per_stream;
+  FastDiv groups;      // workgroups of a stream (set by the launcher)
+  int rows, D;
+  double eps;
+  int8_t* codes;
+  int64_t ldc;
+  float* scales;
+};
+hipError_t launch_int_norm(hipStream_t st, IntNormArgs a);
+
+// y[M][N] = epilogue(sx[i] sw[j] sum_k X[i][k] W[j][k]); rows of X and W 16-byte aligned.
+struct IntGemmArgs {
+  const int8_t* x;
+  int64_t ldx;
+  const float* sx;
+  const int8_t* w;
+  int64_t ldw;
+  const float* sw;
+  int M, N, K;
+  const bf16_t* bias;   // or null
+  const void* res;      // with kEpiBiasRes, kEpiBiasGateRes
+  bool res_f32;
+  int64_t ldr;
+  const float* mod;     // with kEpiBiasGateRes: [streams][6][N]
+  const float* table;   // [6][N] or null
+  int gate_row;
+  FastDiv rows_per_stream;
+  void* y;
+  bool y_f32;
+  int64_t ldy;
+};
+hipError_t launch_int_gemm(hipStream_t st, int epi, const IntGemmArgs& a);
+
 }  // namespace ardit
