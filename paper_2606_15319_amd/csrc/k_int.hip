@@ -381,7 +381,9 @@ __global__ __launch_bounds__(64 * kNormRows) void int_norm_kernel(const IntNormA
   const bool finite = top < kInfBits;
   // (where ym is 0 the largest |y| is below 2^-149, and its scale rounds to 0)
 
-  // element j of the row again, in fp64
+  // element j of the row again, in fp64; without scale and shift in units of 1 / rms, which the
+  // codes do not depend on: h gain is exact, and so are its halves of the largest
+  const bool in_units = !has_b && p.a_row < 0;
   auto again = [&](int j) -> double {
     float z;
     if (p.h) {
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(64 * kNormRows) void int_norm_kernel(const IntNormA
       }
     }
     const int at = (j & 4) * n8 + 4 * (j >> 3) + (j & 3);
-    double y = static_cast<double>(z) * rs;
+    double y = in_units ? static_cast<double>(z) : static_cast<double>(z) * rs;
     if (has_a) {
       const double a = reinterpret_cast<const float*>(lds_a)[at];
       y *= p.gain ? a : 1.0 + a;
@@ -443,7 +445,7 @@ __global__ __launch_bounds__(64 * kNormRows) void int_norm_kernel(const IntNormA
       cr[c] = q;
     }
   }
-  if (lane == 0) p.scales[row] = finite ? static_cast<float>(m / 127.0) : __uint_as_float(0x7fc00000u);
+  if (lane == 0) p.scales[row] = finite ? static_cast<float>((in_units ? m * rs : m) / 127.0) : __uint_as_float(0x7fc00000u);
   while (open) {
     const int c = lane + 64 * (__ffs(open) - 1);
     open &= open - 1;

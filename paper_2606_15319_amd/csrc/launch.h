@@ -378,8 +378,8 @@ struct IntGemmArgs {
   void* y;
   bool y_f32;
   int64_t ldy;
-  // set by the launcher: four neighbours of a row may be read or written at once
-  bool vec_cols, vec_res, vec_y;   // (per-column vectors; residual; y)
+  // set by the launcher: neighbours of a row that may be read or written at once (4, 2 or 1)
+  int width_cols, width_res, width_y;   // (per-column vectors; residual; y)
 };
 hipError_t launch_int_gemm(hipStream_t st, int epi, const IntGemmArgs& a);
 

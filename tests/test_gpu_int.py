@@ -203,6 +203,27 @@ def test_norm_of_a_sum(A, rows, dim, pad, by, per, f32, delta, gate):
     _check_norm(A, rows, dim, f32=f32, delta=delta, gate=gate, by=by, per=per, pad=pad, kind="loud")
 
 
+def test_norm_halves_go_to_the_even_code(A):
+    """With a gain or alone the codes are those of h gain, exactly: a half of the largest is 63.5, and becomes 64."""
+    import torch
+    rng = np.random.default_rng(9)
+    rows, D = 200, 512
+    h = bf16_round(rng.standard_normal((rows, D)).astype(np.float32)).astype(np.float32)
+    gain = bf16_round((1 + 0.1 * rng.standard_normal(D)).astype(np.float32)).astype(np.float32)
+    gain[[0, 1]] = gain[2]
+    h[:, 2] = np.abs(h * gain).max(1) * 2
+    h = bf16_round(h).astype(np.float32)
+    h[:, 0], h[:, 1] = h[:, 2] / 2, -h[:, 2] / 2
+    for g in (gain, None):
+        c = Codes(rows, D)
+        xd, gd = dev_bf16(h), dev_bf16(gain)
+        A.ardit_int_norm(None, rows, D, A.norm_desc(xd, A.BF16, D, gain=gd if g is not None else None), c.q, D, c.s)
+        q, _ = c.host()
+        want, _, _ = I.quantize(h.astype(np.float64) * (gain if g is not None else 1.0))
+        assert np.array_equal(q, want)
+        assert (q[:, 0] == np.sign(h[:, 2]) * 64).all() and (q[:, 1] == -np.sign(h[:, 2]) * 64).all()
+
+
 @pytest.mark.parametrize("over", ["x", "delta"])
 def test_norm_in_place(A, over):
     _check_norm(A, 13, 640, f32=True, delta="f32", gate=True, by="mod", per=4, over=over)
