@@ -349,7 +349,8 @@ struct IntNormArgs {
   const float* table;  // [6][D] or null
   int a_row, shift_row, gate_row;   // rows of the modulation, -1: none
   int64_t rows_per_stream;
-  FastDiv groups;      // workgroups of a stream (set by the launcher)
+  FastDiv groups;      // workgroups of a stream (set by the launcher, like vec_mod)
+  bool vec_mod;        // the modulation's rows are 16-byte vectors
   int rows, D;
   double eps;
   int8_t* codes;
