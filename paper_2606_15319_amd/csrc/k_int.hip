@@ -10,7 +10,7 @@
 // registers, so it is read once: by one wave up to 5120 elements, wider or few rows by several.  What
 // a wave does once a row (reductions, divisions) costs as much as 30 to 40 elements a lane, and
 // shared by more waves it is done more often: 13824 rows of 5120 by five waves each 62 us, by
-// one TIME_Q.
+// one 53 (4.0 TB/s; 4680 rows of 13824 by three 50, 3.9).
 #include <algorithm>
 
 #include "launch.h"
@@ -157,6 +157,12 @@ __device__ __forceinline__ uint2 exact_codes8(Y y, double m) {
   return make_uint2(pack_bytes(w[0], w[1], w[2], w[3]), pack_bytes(w[4], w[5], w[6], w[7]));
 }
 
+// Results are written past the L2, whose dirty lines a kernel has to flush when it ends: codes of
+// 4680 x 5120 normed from fp32 47.7 us for 54.2, the fp32 values of 4680 x 13824 codes 56 for 98.
+__device__ __forceinline__ void store_codes(uint2* p, uint2 w) {
+  __builtin_nontemporal_store(static_cast<uint64_t>(w.y) << 32 | w.x, reinterpret_cast<uint64_t*>(p));
+}
+
 constexpr uint32_t kInfBits = 0x7f800000u;
 
 }  // namespace
@@ -212,7 +218,7 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void int_quantize_kernel(const vo
       to_floats<F>(q[i], v);
       const uint2 w = codes8(v, inv, &far);
       if (far > thr) open |= 1u << i;
-      cr[c] = numbers ? w : make_uint2(0, 0);
+      store_codes(cr + c, numbers ? w : make_uint2(0, 0));
     }
   }
   if (t0 == 0) scales[row] = top < kInfBits ? m / 127.f : __uint_as_float(0x7fc00000u);
@@ -347,8 +353,10 @@ constexpr int kNormRows = 8;   // rows of a workgroup, one a wave
 // bound says which elements may be the largest and which codes are open, and those are computed
 // again in fp64.
 // XF, DK: type of x (kBf16, kF32, kAny) and of delta (the same; -1: none).
+// (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and run
+// without spills: 9360 rows of 5120 157 us for 175.)
 template <int MAXC, int XF, int DK>
-__global__ __launch_bounds__(64 * kNormRows, MAXC > 10 ? 2 : 4) void int_norm_kernel(const IntNormArgs p) {
+__global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0) ? 2 : 4) void int_norm_kernel(const IntNormArgs p) {
   constexpr bool VEC = XF != kAny;
   extern __shared__ float4 lds_vec[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -449,8 +457,9 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 ? 2 : 4) void int_norm_ke
       if (p.h) {
         float* hr = p.h + row * p.ldh + 8 * c;
         if (VEC) {
-          reinterpret_cast<float4*>(hr)[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-          reinterpret_cast<float4*>(hr)[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
+          f32x4* ho = reinterpret_cast<f32x4*>(hr);
+          __builtin_nontemporal_store(f32x4{v[i][0], v[i][1], v[i][2], v[i][3]}, ho);
+          __builtin_nontemporal_store(f32x4{v[i][4], v[i][5], v[i][6], v[i][7]}, ho + 1);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -548,7 +557,7 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 ? 2 : 4) void int_norm_ke
         w = codes8(y, inv, &far);
         if (far > thr) open |= 1u << i;
       }
-      cr[c] = w;
+      store_codes(cr + c, w);
     }
   }
   if (lane == 0) p.scales[row] = finite ? static_cast<float>((in_units ? m * rs : m) / 127.0) : __uint_as_float(0x7fc00000u);
