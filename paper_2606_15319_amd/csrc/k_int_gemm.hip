@@ -74,10 +74,12 @@ __device__ __forceinline__ void load4(const T* p, int left, int width, float* f)
     for (int e = 0; e < 4; ++e) f[e] = e < left ? as_float(p[e]) : 0.f;
   }
 }
+// (fp32 results go past the L2: 4680 x 5120 of them 147 us for 161 with the residual's read, 4680 x
+// 1536 26 for 33; bf16 ones, whose lines fill in pieces of 32 bytes, take longer that way, 117 for 101.)
 template <typename T>
 __device__ __forceinline__ void store4(T* p, int left, int width, const float* y) {
   if (width == 4 && left >= 4) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+    if constexpr (sizeof(T) == 4) __builtin_nontemporal_store(f32x4{y[0], y[1], y[2], y[3]}, reinterpret_cast<f32x4*>(p));
     else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
   } else if (width >= 2 && left >= 4) {
 #pragma unroll
@@ -639,22 +641,23 @@ static void launch_split(hipStream_t st, int epi, const IntGemmArgs& a) {
 
 // The kernel of a product of more than 64 rows, by its estimated end (us):
 //   start + rounds (fixed + steps (step + load fill))
-// with the tiles over the CUs' places (256; two of the 64 x 64 tiles share a CU, and
-// are counted by half rounds), `fill` the share of them taken, and K in steps of 128.  The constants are
-// fitted to warm calls of one card; estimate and measurement of the taken kernel and of the next
-// best, M x N x K: 128 x 1536 x 8960 16.1 / 16.0 (32 x 64), 21.4 / 21.5; 512 x 1536 x 1536 7.3 / 6.9
-// (64 x 64 in two groups), 7.4 / 7.4; 256 x 5120 x 5120 18.5 / 18.0 (64 x 128 in two groups), 23.8 /
-// 22.2; 512 x 5120 x 5120 28.3 / 28.9 (128 x 128), 33.4 / 34.2; 1560 x 4608 x 1536 17.0 / 18.4 (128 x
-// 256), 19.5 / 21.7; 4680 x 5120 x 13824 241 / 252 (192 x 256), 289 / 280; 16384 x 8192 x 8192 767 /
-// 795 (256 x 256), 806 / 831.
+// with the tiles over the CUs' places (256; two of the 64 x 64 tiles share a CU, and are counted by
+// half rounds), `fill` the share of the places taken, and K in steps of 128.  The constants are
+// fitted to warm calls of one card.  Estimate and measurement of the kernel taken and of the next
+// best, M x N x K: 128 x 1536 x 8960 16.1 / 15.7 (32 x 64), 21.4 / 21.6; 300 x 2600 x 700 5.4 / 5.4
+// (64 x 64), 6.5 / 7.0; 512 x 1536 x 1536 7.3 / 6.8 (64 x 64 in two groups), 7.4 / 7.3; 256 x 5120 x
+// 5120 18.4 / 17.9 (64 x 128 in two groups), 24.0 / 21.6; 512 x 5120 x 5120 28.3 / 29.0 (128 x 128),
+// 34.5 / 34.5; 1560 x 4608 x 1536 17.0 / 17.8 (128 x 256), 18.7 / 21.1; 4680 x 5120 x 13824 241 / 253
+// (192 x 256), 289 / 272; 16384 x 8192 x 8192 767 / 785 (256 x 256), 808 / 826.  Of 45 products
+// measured on all of them it takes the fastest of 36, and loses at most 1.2 us or 17% of the others.
 enum Tile { kT32x64, kT64x64, kT64x64Pair, kT64x128, kT128x128, kT128x256, kT192x256, kT256x256, kTiles };
 static Tile choose_tile(int M, int N, int K) {
   struct Cost {
     int m, n;
     double start, fixed, step, load;
   };
-  static const Cost cost[kTiles] = {{32, 64, 2.5, 0.5, 0.15, 0.10},   {64, 64, 3.3, 0, 0.345, 0},
-                                    {64, 64, 3.0, 1.2, 0.24, 0.03},   {64, 128, 3.0, 1.2, 0.33, 0.04},
+  static const Cost cost[kTiles] = {{32, 64, 1.5, 1.5, 0.15, 0.10},   {64, 64, 2.3, 1.0, 0.345, 0},
+                                    {64, 64, 1.7, 2.5, 0.24, 0.03},   {64, 128, 1.7, 2.5, 0.33, 0.04},
                                     {128, 128, 3.0, 3.0, 0.52, 0.06}, {128, 256, 3.0, 3.5, 0.61, 0.29},
                                     {192, 256, 3.0, 6.5, 0.70, 0.35}, {256, 256, 3.0, 8.5, 0.91, 0.45}};
   const int steps = (K + 127) / 128;

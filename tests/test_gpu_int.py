@@ -341,10 +341,22 @@ def test_linear_long(A, M, N, K):
     _linear_case(A, M, N, K, out="f32", ends=True, bias=False)
 
 
-@pytest.mark.parametrize("M,N,K", [(2500, 640, 256), (1400, 1990, 336), (4680, 300, 128), (1000, 5120, 144)])
-def test_linear_large(A, M, N, K):
+# sizes that reach every tile of the large products, with steps of K from one to many and cut short
+@pytest.mark.parametrize("M,N,K", [(130, 129, 1000), (389, 1280, 640), (500, 1500, 1600), (300, 5000, 2000),
+                                   (2000, 1990, 1315), (1000, 5120, 144), (1500, 4500, 300), (3000, 5000, 128),
+                                   (2400, 4000, 272), (4000, 2600, 260), (9000, 3900, 200), (2890, 5125, 400),
+                                   (2800, 5120, 1290), (2500, 640, 256), (4680, 300, 128)])
+def test_linear_tiles(A, M, N, K):
     _linear_case(A, M, N, K, epi="gate", out="bf16", per=1000)
-    _linear_case(A, M, N, K, out="f32", bias=False)
+    _linear_case(A, M, N, K, out="f32", bias=False, pad=1)
+
+
+# one to four blocks of 16 columns a workgroup, over more and fewer steps of K than it has waves
+@pytest.mark.parametrize("K", [150, 1300])
+@pytest.mark.parametrize("M", [1, 16, 20, 50, 64])
+@pytest.mark.parametrize("N", [4000, 4100, 8200, 12300, 17001])
+def test_linear_few_rows(A, M, N, K):
+    _linear_case(A, M, N, K, epi="res", out="f32", res="f32")
 
 
 def test_linear_scales_at_their_ends(A):
