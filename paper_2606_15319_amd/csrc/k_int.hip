@@ -3,8 +3,8 @@
 // A row y with m = max|y| takes the scale m / 127 and the codes rint(127 y / m), decided exactly:
 // the fp32 estimate t = y (127 / m) is off by a bound that the kernel knows, so only elements
 // whose t lies that near to a half (a few in 10^5) are decided again in fp64, by the sign of
-// 254 |y| - (2 k + 1) m, with the other seven of their chunk, which is read again for that (the
-// code for it stays out of the way: unrolled over a row in registers it fills the caches).
+// 254 |y| - (2 k + 1) m.  Their chunks of 8 are read again for that (unrolled over a row in registers
+// the code for it would fill the caches).
 //
 // All are bound by HBM (quantising reads 2 or 4 bytes an element and writes 1).  A row is held in
 // registers, so it is read once: by one wave up to 5120 elements, wider or few rows by several.  What
@@ -134,31 +134,37 @@ __device__ __forceinline__ uint2 codes8(const float* y, float inv, float* far) {
   return make_uint2(pack_bytes(w[0], w[1], w[2], w[3]), pack_bytes(w[4], w[5], w[6], w[7]));
 }
 
-// The code of y in a row whose largest magnitude is m > 0.
-__device__ __forceinline__ int exact_code(double y, double m) {
+// The code of y in a row whose largest magnitude is m > 0; k_known: a whole number below 127 |y| / m
+// that the code is at or one above, or -1 for unknown.
+__device__ __forceinline__ int exact_code(double y, double m, float k_known) {
 #pragma clang fp contract(off)   // (both products of `side` rounded alike, so that halves of m tie)
   const double a = fabs(y);
-  double k = floor(127.0 * (a / m));   // (or one off: the border decides)
+  double k = k_known;
+  if (k_known < 0.f) k = floor(127.0 * (a / m));   // (or one off: the border decides)
   const double side = 254.0 * a - (2.0 * k + 1.0) * m;
   if (side > 0.0 || (side == 0.0 && (static_cast<int>(k) & 1))) k += 1.0;
   const int q = static_cast<int>(k);
   return y < 0.0 ? -q : q;
 }
 
-// Codes of eight elements y(e), one after the other (side by side they take many registers).
+// codes8 with the open elements (all where inv is no number, and thr -1) decided from exact(e).
 template <typename Y>
-__device__ __forceinline__ uint2 exact_codes8(Y y, double m) {
+__device__ __forceinline__ uint2 settled8(const float* y, float inv, float thr, Y exact, double m) {
   uint32_t w[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    w[e] = static_cast<uint32_t>(exact_code(y(e), m));
-    __builtin_amdgcn_sched_barrier(0);
+    const float r = fmaf(y[e], inv, kMagic);
+    w[e] = __float_as_uint(r);
+    // (thr >= 0: t is less than a half off, so the code is |t|'s floor or one above)
+    if (!(fabsf(fmaf(y[e], inv, kMagic - r)) <= thr))
+      w[e] = static_cast<uint32_t>(exact_code(exact(e), m, thr < 0.f ? -1.f : floorf(fabsf(y[e] * inv))));
   }
   return make_uint2(pack_bytes(w[0], w[1], w[2], w[3]), pack_bytes(w[4], w[5], w[6], w[7]));
 }
 
-// Results are written past the L2, whose dirty lines a kernel has to flush when it ends: codes of
-// 4680 x 5120 normed from fp32 47.7 us for 54.2, the fp32 values of 4680 x 13824 codes 56 for 98.
+// Results are written past the L2, whose dirty lines a kernel has to flush when it ends: with plain
+// stores the norm of 4680 x 5120 from fp32 takes 6.5 us longer, and the fp32 values of
+// 4680 x 13824 codes 98 us for 56.
 __device__ __forceinline__ void store_codes(uint2* p, uint2 w) {
   __builtin_nontemporal_store(static_cast<uint64_t>(w.y) << 32 | w.x, reinterpret_cast<uint64_t*>(p));
 }
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(ONE ? 256 : 1024) void int_quantize_kernel(const vo
     if (8 * c < cols) load_chunk<F>(xr, f32, c, cols, again);
     float v[8];
     to_floats<F>(again, v);
-    cr[c] = exact_codes8([&](int e) { return static_cast<double>(v[e]); }, m);
+    cr[c] = settled8(v, inv, thr, [&](int e) { return static_cast<double>(v[e]); }, m);
   }
 }
 
@@ -354,7 +360,7 @@ constexpr int kNormRows = 8;   // rows of a workgroup, one a wave
 // again in fp64.
 // XF, DK: type of x (kBf16, kF32, kAny) and of delta (the same; -1: none).
 // (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and run
-// without spills: 9360 rows of 5120 157 us for 175.)
+// without spills: 9360 rows of 5120 149 us (4.9 TB/s), with spills 18 more.)
 template <int MAXC, int XF, int DK>
 __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0) ? 2 : 4) void int_norm_kernel(const IntNormArgs p) {
   constexpr bool VEC = XF != kAny;
@@ -575,7 +581,9 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
       if (has_d) load_chunk<DF>(dr, d_f32, c, D, d);
       sum8(x, d, c, h);
     }
-    cr[c] = exact_codes8([&](int e) { return exact(h[e], c, e); }, m);
+    float y[8];
+    form(h, c, y, nullptr);
+    cr[c] = settled8(y, inv, thr, [&](int e) { return exact(h[e], c, e); }, m);
   }
 }
 
