@@ -330,7 +330,8 @@ int ardit_attn_fwd_mx(hipStream_t stream, const ardit_dims* dims, const ardit_ba
  * calls that write codes write zeros from cols up to the next multiple of 16 and nothing past
  * that.  Zero rows (and only then NULL buffers) are allowed: nothing is done.  Rows of other
  * tensors may start anywhere an element may (16-byte aligned bases with strides of 16 bytes
- * run faster); strides are in elements and at least the row's length. */
+ * run faster); strides are in elements and at least the row's length.  What a call writes overlaps
+ * nothing that it reads, but where its descriptor says so. */
 
 /* Element type of a tensor argument. */
 typedef enum { ARDIT_BF16 = 0, ARDIT_F32 = 1 } ardit_type;
@@ -351,7 +352,9 @@ int ardit_int_dequantize(hipStream_t stream, const void* codes, int64_t rows, in
  *   u   = h / sqrt(mean(h^2) + eps)
  *   y   = u * gain  |  u * (1 + V_scale) + V_shift (scale_row or shift_row -1: without)  |  u
  * and the codes of y.  (In a block: the gated residual's addition and adaLN, or the
- * cross-attention's pre-norm.)  Sums are fp64, codes exact as above. */
+ * cross-attention's pre-norm.)  Sums are fp64, codes exact as above.  h, V and y past fp32's range
+ * are infinities; a row whose largest y is nearer to 0 than to 2^-149 may have zero codes (its
+ * scale rounds to 0 with any). */
 typedef struct {
   const void* x;            /* [rows][dim], x_type, stride ldx: the residual stream */
   int32_t x_type;
@@ -367,7 +370,7 @@ typedef struct {
   const float* mod_table;   /* [6][dim], or NULL */
   int32_t shift_row, scale_row, gate_row;   /* 0 .. 5, or -1 for none */
   int64_t rows_per_stream;  /* >= 1; read where a row is named */
-  double eps;               /* > 0 */
+  double eps;               /* 1e-70 (1 / sqrt of it is an fp32 number) .. 1e300 */
 } ardit_norm_desc;
 
 /* The norm of a linear layer's input with the residual's addition before it and its output in

@@ -1514,7 +1514,8 @@ int ardit_int_norm(hipStream_t stream, int64_t rows, int32_t dim, const ardit_no
     if (norm->shift_row >= 0 || norm->scale_row >= 0)
       return fail(ARDIT_EINVAL, "gain together with shift or scale");
   }
-  if (!(norm->eps > 0.0) || !(norm->eps <= 1e300)) return fail(ARDIT_EINVAL, "eps must be positive");
+  // (the kernel's estimates hold 1 / rms in fp32)
+  if (!(norm->eps >= 1e-70) || !(norm->eps <= 1e300)) return fail(ARDIT_EINVAL, "eps must be in [1e-70, 1e300]");
   ARDIT_TRY(check_codes(codes, ldc, scales, dim, none, "codes"));
   if (none) return ARDIT_OK;
   IntNormArgs a = {};

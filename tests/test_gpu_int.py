@@ -238,6 +238,30 @@ def test_norm_of_unusual_rows(A, kind, by, f32):
     _check_norm(A, 10, 77, f32=f32, by=by, kind=kind, keep=False, table=False)
 
 
+@pytest.mark.parametrize("kind", ["odd", "tiny", "huge"])
+@pytest.mark.parametrize("by", ["gain", "mod", "plain", "shift"])
+@pytest.mark.parametrize("eps", [1e-70, 1e4])
+def test_norm_with_the_ends_of_eps(A, kind, by, eps):
+    """Rows of zeros and of subnormal numbers beside 1 / rms at both ends."""
+    _check_norm(A, 10, 384, f32=True, by=by, kind=kind, keep=False, eps=eps)
+
+
+def test_norm_too_small_for_a_scale(A):
+    """1 / rms of 1e-150: y is 0 in 32 bits, so the scale is; with a shift y is the shift."""
+    x = np.random.default_rng(4).standard_normal((7, 300)).astype(np.float32)
+    mod = np.random.default_rng(5).standard_normal((1, 6, 300)).astype(np.float32)
+    xd, md = dev_f32(x), dev_f32(mod)
+    c = Codes(7, 300)
+    A.ardit_int_norm(None, 7, 300, A.norm_desc(xd, A.F32, 300, eps=1e300), c.q, c.ld, c.s)
+    assert (c.host()[1] == 0.0).all()
+    A.ardit_int_norm(None, 7, 300, A.norm_desc(xd, A.F32, 300, mod=md, rows_per_stream=7, shift_row=3, eps=1e300),
+                     c.q, c.ld, c.s)
+    q, s = c.host()
+    want, ws, margin = I.quantize(np.broadcast_to(mod[:, 3], (7, 300)).astype(np.float64))
+    assert np.array_equal(q[margin > 1e-9], want[margin > 1e-9])
+    assert (np.abs(s.astype(np.float64) - ws) <= np.spacing(ws)).all()
+
+
 def test_norm_whose_terms_cancel(A):
     """Shift against scale: y is small beside its terms, where fp32 alone would take other codes."""
     import torch

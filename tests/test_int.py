@@ -120,7 +120,8 @@ def test_dequantize_refuses(change, status):
     (dict(gate_row=2, mod=FAKE), EINVAL),                         # no delta
     (dict(scale_row=1, mod=FAKE, rows_per_stream=0), EINVAL), (dict(scale_row=1, mod=FAKE + 2), EINVAL),
     (dict(scale_row=1, mod=FAKE, gain=FAKE), EINVAL), (dict(scale_row=1, mod=FAKE, mod_table=FAKE + 1), EINVAL),
-    (dict(gain=FAKE + 1), EINVAL), (dict(eps=0.0), EINVAL), (dict(eps=float("nan")), EINVAL)])
+    (dict(gain=FAKE + 1), EINVAL), (dict(eps=0.0), EINVAL), (dict(eps=float("nan")), EINVAL),
+    (dict(eps=1e-71), EINVAL), (dict(eps=1e301), EINVAL), (dict(eps=-1e-6), EINVAL)])
 def test_norm_refuses(change, status):
     a = dict(x=FAKE, x_type=A.BF16, ldx=100)
     a.update(change)
