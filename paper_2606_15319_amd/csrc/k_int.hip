@@ -6,11 +6,12 @@
 // 254 |y| - (2 k + 1) m.  Their chunks of 8 are read again for that (unrolled over a row in registers
 // the code for it would fill the caches).
 //
-// All are bound by HBM (quantising reads 2 or 4 bytes an element and writes 1).  A row is held in
-// registers, so it is read once: by one wave up to 5120 elements, wider or few rows by several.  What
-// a wave does once a row (reductions, divisions) costs as much as 30 to 40 elements a lane, and
-// shared by more waves it is done more often: 13824 rows of 5120 by five waves each 62 us, by
-// one 53 (4.0 TB/s; 4680 rows of 13824 by three 50, 3.9).
+// Quantising (2 or 4 bytes read an element, 1 written) and reading back are bound by HBM; the norm by its chain
+// of dependent steps too (1.9 to 3.5 TB/s).  A row is held in registers, so it is read once: by one wave up
+// to 5120 elements when quantised and always when normed, wider or few rows by several.  What a wave does
+// once a row (reductions, divisions) costs as much as 30 to 40 elements a lane, and shared by more
+// waves it is done more often: 13824 rows of 5120 quantised by five waves each 62 us, by one 53
+// (4.0 TB/s; 4680 rows of 13824 by three 50, 3.9).
 #include <algorithm>
 
 #include "launch.h"
@@ -360,7 +361,9 @@ constexpr int kNormRows = 8;   // rows of a workgroup, one a wave
 // again in fp64.
 // XF, DK: type of x (kBf16, kF32, kAny) and of delta (the same; -1: none).
 // (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and run
-// without spills: 9360 rows of 5120 149 us (4.9 TB/s), with spills 18 more.)
+// without spills: 9360 rows of 5120 149 us (3.5 TB/s), with spills 18 more.  Its eight waves a CU load, sum and
+// store in turn; going from row to row in a loop, with the next row requested ahead or not, spills and
+// takes 187 to 195.  Four rows a workgroup take as long, sixteen 20 to 30% longer.)
 template <int MAXC, int XF, int DK>
 __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0) ? 2 : 4) void int_norm_kernel(const IntNormArgs p) {
   constexpr bool VEC = XF != kAny;
