@@ -352,9 +352,9 @@ int ardit_int_dequantize(hipStream_t stream, const void* codes, int64_t rows, in
  *   u   = h / sqrt(mean(h^2) + eps)
  *   y   = u * gain  |  u * (1 + V_scale) + V_shift (scale_row or shift_row -1: without)  |  u
  * and the codes of y.  (In a block: the gated residual's addition and adaLN, or the
- * cross-attention's pre-norm.)  Sums are fp64, codes exact as above.  h, V and y past fp32's range
- * are infinities; a row whose largest y is nearer to 0 than to 2^-149 may have zero codes (its
- * scale rounds to 0 with any). */
+ * cross-attention's pre-norm.)  Sums are fp64, codes exact as above: u and 1 / sqrt may lie below
+ * fp32's normal numbers.  h, V and y past fp32's range are infinities; a row whose m / 127 is nearer to
+ * 0 than to 2^-149 has its codes and the scale 0. */
 typedef struct {
   const void* x;            /* [rows][dim], x_type, stride ldx: the residual stream */
   int32_t x_type;

@@ -171,6 +171,7 @@ __device__ __forceinline__ void store_codes(uint2* p, uint2 w) {
 }
 
 constexpr uint32_t kInfBits = 0x7f800000u;
+constexpr uint32_t kWideBits = 0x49800000u;   // 2^20
 
 }  // namespace
 
@@ -356,9 +357,10 @@ constexpr int kNormRows = 8;   // rows of a workgroup, one a wave
 // A workgroup's rows belong to one stream, whose vectors (gate, shift, scale or gain) are staged in
 // LDS as fp32 with the halves of every chunk apart, so that a wave's 16-byte reads are
 // consecutive.  The mean square is summed in fp64, and the fp32 estimate of
-// y = p + shift, p = (h rs) (1 + scale), is within 2^-24 (3 max|p| + max|y|) of the truth: that
-// bound says which elements may be the largest and which codes are open, and those are computed
-// again in fp64.
+// y = p + shift, p = (h rs) (1 + scale), is within 2^-24 (3 max|p| + max|y|) of the truth, and where
+// h rs is subnormal 2^-150 |1 + scale| more, below 2^-129 for scales up to 2^20: that bound says which
+// elements may be the largest and which codes are open, and those are computed again in fp64.  With
+// larger vectors, or rs below fp32's normal numbers, all are.
 // XF, DK: type of x (kBf16, kF32, kAny) and of delta (the same; -1: none).
 // (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and run
 // without spills: 9360 rows of 5120 149 us (3.5 TB/s), with spills 18 more.  Its eight waves a CU load, sum and
@@ -399,7 +401,7 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
   float4* lds_a = lds_vec;
   float4* lds_b = lds_a + (has_a ? 2 * n8 : 0);
   float4* lds_g = lds_b + (has_b ? 2 * n8 : 0);
-  float poor = 0.f;   // stays 0 unless an infinity or a NaN is in the vectors: it is then in every row
+  uint32_t widest = 0;   // bits of the vectors' largest magnitude: an infinity or a NaN is then in every row
   auto stage = [&](float4* to, int r) __attribute__((always_inline)) {
     const float* m = p.mod + (static_cast<int64_t>(b) * 6 + r) * D;
     const float* t = p.table ? p.table + static_cast<int64_t>(r) * D : nullptr;
@@ -413,7 +415,8 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = 4 * k + e < D ? (t ? m[4 * k + e] + t[4 * k + e] : m[4 * k + e]) : 0.f;
       }
-      poor = fmaf(f[0], 0.f, fmaf(f[1], 0.f, fmaf(f[2], 0.f, fmaf(f[3], 0.f, poor))));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) widest = max(widest, abs_bits(f[e]));
       to[(k & 1) * n8 + (k >> 1)] = make_float4(f[0], f[1], f[2], f[3]);
     }
   };
@@ -422,7 +425,8 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
       float f[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] = 4 * k + e < D ? bf2f(p.gain[4 * k + e]) : 0.f;
-      poor = fmaf(f[0], 0.f, fmaf(f[1], 0.f, fmaf(f[2], 0.f, fmaf(f[3], 0.f, poor))));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) widest = max(widest, abs_bits(f[e]));
       lds_a[(k & 1) * n8 + (k >> 1)] = make_float4(f[0], f[1], f[2], f[3]);
     }
   } else if (has_a) {
@@ -430,7 +434,8 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
   }
   if (has_b) stage(lds_b, p.shift_row);
   if (has_g) stage(lds_g, p.gate_row);
-  const bool spoilt = __syncthreads_or(!(poor == 0.f));
+  const bool wide = __syncthreads_or(widest >= kWideBits);
+  const bool spoilt = wide && __syncthreads_or(widest >= kInfBits);
   if (!live) return;
   auto vec8 = [&](const float4* v, int c, float* f) __attribute__((always_inline)) {
     const float4 lo = v[c], hi = v[n8 + c];
@@ -529,16 +534,14 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
   // (maxima of non-negative numbers as those of their bits; a NaN in h shows in the sum)
   const float ym = __uint_as_float(wave_max(__float_as_uint(most)));
   pm = has_b ? __uint_as_float(wave_max(__float_as_uint(pm))) : ym;
-  // error of y; of a subnormal 1 / rms nothing is known
-  float err = 5.97e-8f * (3.25f * pm + 1.25f * ym) + 1e-44f;
-  if (!(rs32 > 3e-38f)) err = ym + 1.f;
+  const bool known = !wide && rs32 > 3e-38f;   // else nothing is known of y
+  const float err = 5.97e-8f * (3.25f * pm + 1.25f * ym) + 3e-39f;
   const bool finite = !spoilt && ym <= 3.4028235e38f && ss <= 1.7e308;
-  // (where ym is 0 the largest |y| is below 2^-149, and its scale rounds to 0)
 
   // the largest magnitude, from the chunks that may hold it
   double m = 0.0;
-  if (finite && ym != 0.f) {
-    const float low = ym - 2.f * err;
+  if (finite && (ym != 0.f || ss != 0.0)) {   // (y is 0 throughout where both are)
+    const float low = known ? ym - 2.f * err : -1.f;
     if (most >= low) {
 #pragma unroll
       for (int i = 0; i < MAXC; ++i) {
@@ -552,7 +555,7 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
   }
   const bool numbers = finite && m > 0.0;
   const float inv = numbers ? 127.f / ym : 0.f;
-  const float thr = inv < 3e38f ? 0.5f - 1.1f * (2.f * err * inv + 1.6e-5f) : -1.f;
+  const float thr = known && inv < 3e38f ? 0.5f - 1.1f * (2.f * err * inv + 1.6e-5f) : -1.f;
   uint2* cr = reinterpret_cast<uint2*>(p.codes + row * p.ldc);
   uint32_t open = 0;
 #pragma unroll

@@ -282,6 +282,55 @@ def test_norm_whose_terms_cancel(A):
     assert sure.mean() > 0.999 and np.array_equal(q[sure], want[sure])
 
 
+def _norm_of(A, x, eps, gain=None, scale=None, shift=None):
+    """Codes and scales of rows x (fp32) beside those of the reference, vectors shared by all rows."""
+    rows, D = x.shape
+    mod = np.zeros((1, 6, D), np.float32)
+    kw = {}
+    keep = [dev_f32(x)]
+    if gain is not None:
+        keep.append(dev_bf16(gain))
+        kw.update(gain=keep[-1])
+    if scale is not None:
+        mod[0, 1] = scale
+        kw.update(scale_row=1)
+    if shift is not None:
+        mod[0, 3] = shift
+        kw.update(shift_row=3)
+    keep.append(dev_f32(mod))
+    if scale is not None or shift is not None:
+        kw.update(mod=keep[-1], rows_per_stream=rows)
+    c = Codes(rows, D)
+    A.ardit_int_norm(None, rows, D, A.norm_desc(keep[0], A.F32, D, eps=eps, **kw), c.q, c.ld, c.s)
+    q, s = c.host()
+    with np.errstate(over="ignore"):
+        want, ws, margin = I.quantize(I.norm(x, eps, gain, scale, shift))
+    sure = margin > 1e-9
+    assert np.array_equal(q[sure], want[sure]), (int((q != want)[sure].sum()), int(sure.sum()))
+    assert (np.abs(q.astype(int) - want)[~sure] <= 1).all()
+    assert (np.abs(s.astype(np.float64) - ws) <= np.spacing(ws)).all()
+    return q, s
+
+
+@pytest.mark.parametrize("by", ["gain", "scale", "mod"])
+@pytest.mark.parametrize("h,eps,vec", [(1e-22, 1e40, 1e6), (1e-21, 1e40, 3e5), (1e-43, 1e-6, 3e5), (1e-22, 1e40, 1e10),
+                                       (1e-30, 1e32, 1e30), (1e-26, 1e40, 1e14), (1e30, 1e80, 1.0), (1e30, 1e92, 1.0),
+                                       (1e-20, 1e40, 1e4)])
+def test_norm_whose_unit_is_no_normal_number(A, h, eps, vec, by):
+    """h / rms or 1 / rms below 2^-126, where 32 bits hold few of its bits or none, in rows whose y is a
+    normal number."""
+    rng = np.random.default_rng(12)
+    rows, D = 20, 1024
+    x = (h * rng.standard_normal((rows, D))).astype(np.float32)
+    x[3] = 0.0
+    v = (vec * rng.standard_normal(D)).astype(np.float32)
+    if by == "gain":
+        _norm_of(A, x, eps, gain=bf16_round(v).astype(np.float32))
+    else:
+        shift = (h / eps ** 0.5 * vec * rng.standard_normal(D)).astype(np.float32)
+        _norm_of(A, x, eps, scale=v, shift=shift if by == "mod" else None)
+
+
 # ---------------------------------------------------------------------- linear
 def _linear_case(A, M, N, K, epi="bias", out="bf16", res="f32", per=None, pad=0, seed=0, ends=False, bias=True):
     import torch
