@@ -536,7 +536,8 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
   pm = has_b ? __uint_as_float(wave_max(__float_as_uint(pm))) : ym;
   const bool known = !wide && rs32 > 3e-38f;   // else nothing is known of y
   const float err = 5.97e-8f * (3.25f * pm + 1.25f * ym) + 3e-39f;
-  const bool finite = !spoilt && ym <= 3.4028235e38f && ss <= 1.7e308;
+  // (p of known rows stays far below fp32's end, so y passes it where its estimate does)
+  bool finite = !spoilt && (!known || ym <= 3.4028235e38f) && ss <= 1.7e308;
 
   // the largest magnitude, from the chunks that may hold it
   double m = 0.0;
@@ -552,6 +553,7 @@ __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0)
       }
     }
     m = wave_join(m, [](double a, double c) { return fmax(a, c); });
+    finite = known || static_cast<float>(in_units ? m * rs : m) <= 3.4028235e38f;
   }
   const bool numbers = finite && m > 0.0;
   const float inv = numbers ? 127.f / ym : 0.f;

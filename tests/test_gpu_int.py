@@ -331,6 +331,42 @@ def test_norm_whose_unit_is_no_normal_number(A, h, eps, vec, by):
         _norm_of(A, x, eps, scale=v, shift=shift if by == "mod" else None)
 
 
+@pytest.mark.parametrize("eps", [1e85, 1e300])
+def test_norm_too_small_for_a_scale_has_its_codes(A, eps):
+    """m / 127 of about 1e-44 (a few of fp32's least steps) and of 1e-152 (the scale is 0)."""
+    x = np.random.default_rng(6).standard_normal((9, 300)).astype(np.float32)
+    q, s = _norm_of(A, x, eps)
+    assert (np.abs(q).max(1) == 127).all() and (s == 0).all() == (eps > 1e90)
+
+
+def test_norm_whose_terms_pass_the_range(A):
+    """u (1 + scale) past fp32's largest number, which the shift brings back: y is a number, and has codes.
+    Without the shift, or with one of the other sign, y is an infinity."""
+    rng = np.random.default_rng(21)
+    rows, D = 5, 264
+    x = rng.standard_normal((1, D)).astype(np.float32)
+    x[0, :40] *= 4
+    x = x * np.float32(2.0) ** np.arange(rows, dtype=np.float32)[:, None]
+    u = (x[0].astype(np.float64) / np.sqrt((x[0].astype(np.float64) ** 2).mean()))
+    far = np.argsort(-np.abs(u))[:7]
+    scale = rng.standard_normal(D).astype(np.float32)
+    shift = (1e38 * rng.standard_normal(D)).clip(-2e38, 2e38).astype(np.float32)
+    scale[far] = (5e38 / u[far]).astype(np.float32)       # p = 5e38
+    shift[far] = -3e38 + 1e37 * np.arange(7, dtype=np.float32)
+    _norm_of(A, x, 1e-30, scale=scale, shift=shift)
+    for other in (None, -shift):
+        c = Codes(rows, D)
+        mod = np.zeros((1, 6, D), np.float32)
+        mod[0, 1] = scale
+        if other is not None:
+            mod[0, 3] = other
+        xd, md = dev_f32(x), dev_f32(mod)
+        A.ardit_int_norm(None, rows, D, A.norm_desc(xd, A.F32, D, eps=1e-30, mod=md, rows_per_stream=rows, scale_row=1,
+                                                    shift_row=-1 if other is None else 3), c.q, c.ld, c.s)
+        q, s = c.host()
+        assert np.isnan(s).all() and not q.any()
+
+
 # ---------------------------------------------------------------------- linear
 def _linear_case(A, M, N, K, epi="bias", out="bf16", res="f32", per=None, pad=0, seed=0, ends=False, bias=True):
     import torch
