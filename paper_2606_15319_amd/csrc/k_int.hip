@@ -2,9 +2,9 @@
 //
 // A row y with m = max|y| takes the scale m / 127 and the codes rint(127 y / m), decided exactly:
 // the fp32 estimate t = y (127 / m) is off by a bound that the kernel knows, so only elements
-// whose t lies that near to a half (a few in 10^5) are decided again in fp64, by the sign of
-// 254 |y| - (2 k + 1) m.  Their chunks of 8 are read again for that (unrolled over a row in registers
-// the code for it would fill the caches).
+// whose t lies that near to a half (3 in 10^5 when quantised, 2 in 10^4 when normed, so one in most
+// rows of 5120) are decided again in fp64, by the sign of 254 |y| - (2 k + 1) m.  Their chunks of 8 are
+// read again for that (unrolled over a row in registers the code for it would fill the caches).
 //
 // Quantising (2 or 4 bytes read an element, 1 written) and reading back are bound by HBM; the norm by its chain
 // of dependent steps too (1.9 to 3.5 TB/s).  A row is held in registers, so it is read once: by one wave up
@@ -165,7 +165,7 @@ __device__ __forceinline__ uint2 settled8(const float* y, float inv, float thr, 
 
 // Results are written past the L2, whose dirty lines a kernel has to flush when it ends: with plain
 // stores the norm of 4680 x 5120 from fp32 takes 6.5 us longer, and the fp32 values of
-// 4680 x 13824 codes 98 us for 56.
+// 4680 x 13824 codes 98 us for 56.  (Rows that are no 16-byte vectors, and bf16 values, take plain stores.)
 __device__ __forceinline__ void store_codes(uint2* p, uint2 w) {
   __builtin_nontemporal_store(static_cast<uint64_t>(w.y) << 32 | w.x, reinterpret_cast<uint64_t*>(p));
 }
@@ -254,7 +254,8 @@ static void launch_q(hipStream_t st, const IntRows& r, int waves, int8_t* codes,
 #undef ARDIT_Q
 }
 
-// rows of 16-byte vectors throughout
+// rows of 16-byte vectors throughout; others are loaded and stored by elements (us: 4680 bf16 rows of 13821
+// quantised 132, of 13824 49; 4680 fp32 rows of 5119 normed 106, of 5120 47)
 static bool vec_rows(const void* p, bool f32, int cols, int64_t ld) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols % 8 == 0 && ld * (f32 ? 4 : 2) % 16 == 0;
 }
@@ -362,10 +363,12 @@ constexpr int kNormRows = 8;   // rows of a workgroup, one a wave
 // elements may be the largest and which codes are open, and those are computed again in fp64.  With
 // larger vectors, or rs below fp32's normal numbers, all are.
 // XF, DK: type of x (kBf16, kF32, kAny) and of delta (the same; -1: none).
-// (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and run
-// without spills: 9360 rows of 5120 149 us (3.5 TB/s), with spills 18 more.  Its eight waves a CU load, sum and
-// store in turn; going from row to row in a loop, with the next row requested ahead or not, spills and
-// takes 187 to 195.  Four rows a workgroup take as long, sixteen 20 to 30% longer.)
+// (Up to 128 registers two workgroups share a CU; long rows with a branch to add need more, and up to
+// 5120 elements run without spills: 9360 rows of 5120 149 us (3.5 TB/s), with spills 18 more.  Its eight waves a CU
+// load, sum and store in turn; going from row to row in a loop, with the next row requested ahead or not, spills
+// and takes 187 to 195.  Four rows a workgroup take as long, sixteen 20 to 30% longer.  Above 5120 elements
+// an fp32 x with an fp32 branch, and rows loaded by elements, spill 55 to 58 registers: 9360 rows of 8192 304 us
+// (2.8 TB/s), with the branch in bf16, which spills none, 260 (3.2).)
 template <int MAXC, int XF, int DK>
 __global__ __launch_bounds__(64 * kNormRows, MAXC > 10 || (MAXC >= 8 && DK >= 0) ? 2 : 4) void int_norm_kernel(const IntNormArgs p) {
   constexpr bool VEC = XF != kAny;

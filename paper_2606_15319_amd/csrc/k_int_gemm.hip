@@ -149,7 +149,8 @@ __device__ __forceinline__ void load_gate(const IntGemmArgs& p, int stream, int 
 // gate once where all rows of the wave are one stream's.
 template <int EPI, typename ResT, typename OutT, int MB, int NB_>
 __device__ __forceinline__ void finish_rows(const IntGemmArgs& p, int m0, int n0, const i32x4 (&acc)[MB][NB_]) {
-  constexpr int AHEAD = MB >= 8 ? (EPI == kEpiBiasGateRes ? 1 : 2) : MB < 3 ? MB : 3;   // (by registers)
+  // (by registers: of all, only gated fp32 results of 256 rows spill, four registers)
+  constexpr int AHEAD = MB >= 8 ? (EPI == kEpiBiasGateRes ? 1 : 2) : MB < 3 ? MB : 3;
   RowIn<EPI, ResT, NB_> in[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) load_row<EPI, ResT, NB_>(p, m0 + 16 * i, n0, in[i]);
@@ -649,7 +650,9 @@ static void launch_split(hipStream_t st, int epi, const IntGemmArgs& a) {
 // 5120 18.4 / 17.9 (64 x 128 in two groups), 24.0 / 21.6; 512 x 5120 x 5120 28.3 / 29.0 (128 x 128),
 // 34.5 / 34.5; 1560 x 4608 x 1536 17.0 / 17.8 (128 x 256), 18.7 / 21.1; 4680 x 5120 x 13824 241 / 253
 // (192 x 256), 289 / 272; 16384 x 8192 x 8192 767 / 785 (256 x 256), 808 / 826.  Of 45 products
-// measured on all of them it takes the fastest of 36, and loses at most 1.2 us or 17% of the others.
+// measured on all of them it takes the fastest of 36.  Of the others small ones lose up to 1.2 us; large
+// results of few steps, whose bytes the estimate does not know, up to 19%: 5000 x 5000 x 128 26.0 us for 22.3,
+// 9360 x 1536 x 256 with an fp32 residual 35.1 for 29.5 (both 128 x 256 for 256 x 256).
 enum Tile { kT32x64, kT64x64, kT64x64Pair, kT64x128, kT128x128, kT128x256, kT192x256, kT256x256, kTiles };
 static Tile choose_tile(int M, int N, int K) {
   struct Cost {
