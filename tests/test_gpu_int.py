@@ -339,6 +339,14 @@ def test_norm_too_small_for_a_scale_has_its_codes(A, eps):
     assert (np.abs(q).max(1) == 127).all() and (s == 0).all() == (eps > 1e90)
 
 
+def test_norm_of_subnormal_rows_below_a_scale(A):
+    """1 / rms is a normal number, h / rms 1e-50: 0 in 32 bits throughout, with scales of up to 2^20 too."""
+    x = (1e-40 * np.random.default_rng(7).standard_normal((9, 300))).astype(np.float32)
+    for scale in (None, (1e5 * np.random.default_rng(8).standard_normal(300)).astype(np.float32)):
+        q, s = _norm_of(A, x, 1e20, scale=scale)
+        assert (np.abs(q).max(1) == 127).all() and not s.any()
+
+
 def test_norm_whose_terms_pass_the_range(A):
     """u (1 + scale) past fp32's largest number, which the shift brings back: y is a number, and has codes.
     Without the shift, or with one of the other sign, y is an infinity."""
